@@ -285,12 +285,12 @@ def _fp8(x, pow2):
     rows, cols = x.shape
     g = torch.nn.functional.pad(x.float(), (0, -cols % 128)).view(rows, -1, 128)
     amax = g.abs().amax(2)
+    most = torch.full_like(amax, 448.0)                  # (a division by a number may be a product with its reciprocal)
     if pow2:
-        m, e = torch.frexp(amax / 448.0)
+        m, e = torch.frexp(amax / most)
         sc = torch.ldexp(torch.ones_like(amax), torch.where(m == 0.5, e - 1, e))
         r = 1.0 / sc
     else:
-        most = torch.full_like(amax, 448.0)              # (a division by a number may be a product with its reciprocal)
         sc, r = amax / most, most / amax
     sc, r = torch.where(amax == 0, 1.0, sc), torch.where(amax == 0, 0.0, r)
     return (g * r[..., None]).flatten(1)[:, :cols].to(torch.float8_e4m3fn), sc
