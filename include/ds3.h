@@ -19,8 +19,9 @@
  * power-of-two scaling factors with the scales applied by the matrix
  * instruction, the weight quantizer that also writes the transposed codes,
  * re-tiling of the FP8 activation cache, SwiGLU and RMSNorm fused with their
- * quantizer, the E5M6 cache format, the AdamW step with BF16 moments, and two
- * machine probes for the benchmark.
+ * quantizer, the E5M6 cache format, the AdamW step with BF16 moments; then the
+ * 4-bit (MXFP4) quantizers and products, an expert layer's rows into expert order
+ * and back, and two machine probes for the benchmark.
  *
  * Common rules
  *   - Every data pointer is DEVICE memory owned by the caller.  The library
@@ -505,6 +506,127 @@ ds3_status ds3_dequant_e5m6(const uint8_t* q, int64_t rows, int64_t cols, int64_
 ds3_status ds3_adamw_bf16_states(int64_t n, float* master_w, const float* grad, void* m, void* v, void* w_bf16,
                                  float lr, float beta1, float beta2, float eps, float weight_decay, int64_t step,
                                  void* stream);
+
+/*
+ * MXFP4: 4-bit microscaled operands (the OCP Microscaling format of E2M1 elements
+ * with an E8M0 scale per 32 of them), for weights and activations that are to take
+ * half of FP8's memory and matrix time.  Per group G of 32 consecutive elements
+ *     amax = max |x_i| over G
+ *     s    = the smallest power of two >= amax / 6, at least 2^-127   (1 if amax == 0)
+ *     q_i  = E2M1_round_to_nearest_even(x_i / s)                      (sign always copied)
+ * so nothing saturates; every finite x is allowed.  A group that holds a NaN or an
+ * infinity gets scale byte 255 (E8M0's NaN) and codes of zero: it and every product
+ * with it are NaN.  E2M1: sign, two exponent bits with bias 1, one mantissa bit: 0,
+ * 0.5, 1, 1.5, 2, 3, 4, 6.  Two codes share a byte, the element with the even index in
+ * the low half.  A scale is stored as the byte log2(s) + 127; the bytes of the four
+ * groups of 128 elements are one 32-bit word, the first group's in its low byte:
+ *   word of (row, kb) at s[row * s_stride_row + kb * s_stride_kb], kb = column / 128.
+ * (ceil(cols / 128), 1) is a plain row-major array of scale bytes, (1, rows) the
+ * K-block-major layout the GEMM reads fastest.  A ragged trailing group is simply
+ * smaller, the bytes of groups beyond it are 127.  Leading dimensions of codes are in BYTES.
+ *
+ * ds3_quant_mxfp4:   groups along a row.    q [rows][ldq], s words (row, column / 128)
+ * ds3_quant_mxfp4_t: groups along the rows, written transposed (the operand of a product
+ *                    that contracts over the rows: a weight for the input's gradient,
+ *                    tokens for the weight's).  q_t [cols][ldq], code of (row t, column c)
+ *                    in byte c * ldq + t / 2; s_t word of (column c, block of 128 rows rb) at
+ *                    s_t[c * s_stride_col + rb * s_stride_rb].  `rows` is arbitrary; an odd
+ *                    number of them leaves a code of zero in the last byte's high half.
+ * ds3_dequant_mxfp4: y [rows][ldy] BF16 = decode(q) * s, exact (beyond BF16's range: an infinity).
+ * Alignment: x, y, q 16-byte aligned, ldq % 16 == 0, ldx * sizeof(element), cols *
+ * sizeof(element) (not for the dequantizer: any `cols`) and ldy * 2 multiples of 16 bytes.
+ */
+ds3_status ds3_quant_mxfp4(const void* x, ds3_dtype xt, int64_t rows, int64_t cols, int64_t ldx,
+                           uint8_t* q, int64_t ldq,
+                           uint32_t* s, int64_t s_stride_row, int64_t s_stride_kb, void* stream);
+ds3_status ds3_quant_mxfp4_t(const void* x, ds3_dtype xt, int64_t rows, int64_t cols, int64_t ldx,
+                             uint8_t* q_t, int64_t ldq,
+                             uint32_t* s_t, int64_t s_stride_col, int64_t s_stride_rb, void* stream);
+ds3_status ds3_dequant_mxfp4(const uint8_t* q, int64_t rows, int64_t cols, int64_t ldq,
+                             const uint32_t* s, int64_t s_stride_row, int64_t s_stride_kb,
+                             void* y, int64_t ldy, void* stream);
+
+/*
+ * Product of two MXFP4 matrices, both K-contiguous:
+ *   C[m][n] (+)= sum over k of  (dec(a[m][k]) * sa(m, k / 32)) * (dec(b[n][k]) * sb(n, k / 32))
+ * in FP32, the scales applied by the matrix instruction.
+ *   a [M][lda] codes, b [N][ldb] codes (lda, ldb in bytes), sa, sb scale words as above
+ *   c [M][ldc] BF16 (round to nearest even) or FP32 (ct); accumulate != 0: C += result, FP32 only.
+ * K % 128 == 0; a, b, c 16-byte aligned, lda, ldb % 16 == 0, ldc % 4 == 0; M and N are
+ * arbitrary.  Scale strides are non-negative and reach less than 2^29 words; 257 * lda and
+ * 257 * ldb stay below 2^31 - K / 2.  K == 0 is an empty sum, as in ds3_gemm_fp8_bs.
+ * Results are deterministic; no workspace is needed.
+ *
+ * Grouped over experts as ds3_grouped_gemm_fp8_bs: rows [group_offsets[g], group_offsets[g+1])
+ * of a with b[g]; b [G][N][ldb], scale words of expert g from sb + g * N * (K / 128) on, with
+ * the strides within.  Rows at or beyond group_offsets[G] are left untouched.  G <= 1023, K > 0.
+ */
+ds3_status ds3_gemm_mxfp4(int64_t M, int64_t N, int64_t K,
+                          const uint8_t* a, int64_t lda,
+                          const uint32_t* sa, int64_t sa_stride_row, int64_t sa_stride_kb,
+                          const uint8_t* b, int64_t ldb,
+                          const uint32_t* sb, int64_t sb_stride_row, int64_t sb_stride_kb,
+                          void* c, ds3_dtype ct, int64_t ldc, int accumulate, void* stream);
+ds3_status ds3_grouped_gemm_mxfp4(int32_t G, const int32_t* group_offsets, int64_t total_rows,
+                                  int64_t N, int64_t K,
+                                  const uint8_t* a, int64_t lda,
+                                  const uint32_t* sa, int64_t sa_stride_row, int64_t sa_stride_kb,
+                                  const uint8_t* b, int64_t ldb,
+                                  const uint32_t* sb, int64_t sb_stride_row, int64_t sb_stride_kb,
+                                  void* c, ds3_dtype ct, int64_t ldc, void* stream);
+
+/*
+ * Rows of an expert layer into expert order and back (Section 2.1.2: every token is
+ * computed by the top_k experts its router chose).  A choice is a (token, slot).
+ *
+ * ds3_moe_sort: expert_ids [tokens][ld_ids], `top_k` valid columns; this GPU holds experts
+ * [first_expert, first_expert + G).  Choices of other experts (or any other number, as
+ * padding has) leave no row; a token may choose an expert more than once.
+ *   group_offsets [G+1]            row offsets of the experts' groups, as the grouped GEMMs take them
+ *   row_of_slot   [tokens][top_k]  row of each choice, ordered by (expert, token, slot), or -1
+ * tokens == 0 makes offsets of zero.  top_k <= 64, G <= 1023, tokens * top_k < 2^31.
+ *
+ * ds3_moe_dispatch: x [tokens][ldx]; y[row_of_slot[t][j]] = x[t] for every choice whose row is
+ * in [0, total_rows); other rows of y are left untouched.  y has x's type.  The _quant_ forms
+ * write the row's codes and scales instead, bit for bit those of ds3_quant_act_1x128 (and its
+ * _pow2 form) and ds3_quant_mxfp4 on x[t], with their layouts.
+ *
+ * ds3_moe_combine: out[t] = sum over j of weights[t][j] * y[row_of_slot[t][j]], in FP32, slot
+ * after slot, rounded once; choices without a row in [0, total_rows) add nothing (none at all:
+ * zeros).  weights [tokens][top_k] FP32, or NULL for ones: the gradient of the dispatch.
+ * ds3_moe_combine_bwd: for every choice with a row,
+ *   dy[row] = weights[t][j] * dout[t],   dweights[t][j] = sum over c of dout[t][c] * y[row][c]
+ * in FP32; dweights is 0 for the others, other rows of dy are left untouched.  dy has y's type.
+ * No two choices may name the same row (the sort's never do).
+ *
+ * All matrices 16-byte aligned with rows of whole 16 bytes (cols and ld times the element's
+ * size; codes: ldq % 16 == 0).  The types of y and out / dout are independent.
+ */
+ds3_status ds3_moe_sort(const int32_t* expert_ids, int64_t tokens, int32_t top_k, int64_t ld_ids,
+                        int32_t first_expert, int32_t G,
+                        int32_t* group_offsets, int32_t* row_of_slot, void* stream);
+ds3_status ds3_moe_dispatch(const void* x, ds3_dtype xt, int64_t tokens, int64_t cols, int64_t ldx,
+                            const int32_t* row_of_slot, int32_t top_k, int64_t total_rows,
+                            void* y, int64_t ldy, void* stream);
+ds3_status ds3_moe_dispatch_quant_1x128(const void* x, ds3_dtype xt, int64_t tokens, int64_t cols, int64_t ldx,
+                                        const int32_t* row_of_slot, int32_t top_k, int64_t total_rows,
+                                        uint8_t* q, int64_t ldq,
+                                        float* s, int64_t s_stride_row, int64_t s_stride_kb, void* stream);
+ds3_status ds3_moe_dispatch_quant_1x128_pow2(const void* x, ds3_dtype xt, int64_t tokens, int64_t cols, int64_t ldx,
+                                             const int32_t* row_of_slot, int32_t top_k, int64_t total_rows,
+                                             uint8_t* q, int64_t ldq,
+                                             float* s, int64_t s_stride_row, int64_t s_stride_kb, void* stream);
+ds3_status ds3_moe_dispatch_quant_mxfp4(const void* x, ds3_dtype xt, int64_t tokens, int64_t cols, int64_t ldx,
+                                        const int32_t* row_of_slot, int32_t top_k, int64_t total_rows,
+                                        uint8_t* q, int64_t ldq,
+                                        uint32_t* s, int64_t s_stride_row, int64_t s_stride_kb, void* stream);
+ds3_status ds3_moe_combine(const void* y, ds3_dtype yt, int64_t total_rows, int64_t cols, int64_t ldy,
+                           const int32_t* row_of_slot, const float* weights, int64_t tokens, int32_t top_k,
+                           void* out, ds3_dtype ot, int64_t ldo, void* stream);
+ds3_status ds3_moe_combine_bwd(const void* dout, ds3_dtype ot, int64_t ldo,
+                               const void* y, ds3_dtype yt, int64_t total_rows, int64_t cols, int64_t ldy,
+                               const int32_t* row_of_slot, const float* weights, int64_t tokens, int32_t top_k,
+                               void* dy, int64_t lddy, float* dweights, void* stream);
 
 /*
  * Machine probes for the benchmark (they compute nothing of the method; they

@@ -39,6 +39,9 @@ SYMBOLS = [
     "ds3_grouped_gemm_swiglu_quant_fp8_bs", "ds3_grouped_gemm_swiglu_quant_fp8_bs_pow2",
     "ds3_grouped_gemm_workspace_bytes", "ds3_gemm_few_tiles_config", "ds3_gemm_short_k", "ds3_gemm_between_tile", "ds3_gemm_default_kernel", "ds3_gemm_tail_shared",
     "ds3_grouped_gemm_few_rows_tile",
+    "ds3_quant_mxfp4", "ds3_quant_mxfp4_t", "ds3_dequant_mxfp4", "ds3_gemm_mxfp4", "ds3_grouped_gemm_mxfp4",
+    "ds3_moe_sort", "ds3_moe_dispatch", "ds3_moe_dispatch_quant_1x128", "ds3_moe_dispatch_quant_1x128_pow2",
+    "ds3_moe_dispatch_quant_mxfp4", "ds3_moe_combine", "ds3_moe_combine_bwd",
 ]
 
 
@@ -106,6 +109,17 @@ def _load() -> ctypes.CDLL:
     lib.ds3_gemm_tail_share_steps.restype = i32
     lib.ds3_status_string.argtypes = [i32]
     lib.ds3_status_string.restype = ctypes.c_char_p
+    for name in ("ds3_quant_mxfp4", "ds3_quant_mxfp4_t"):
+        getattr(lib, name).argtypes = [vp, i32, i64, i64, i64, vp, i64, vp, i64, i64, vp]
+    lib.ds3_dequant_mxfp4.argtypes = [vp, i64, i64, i64, vp, i64, i64, vp, i64, vp]
+    lib.ds3_gemm_mxfp4.argtypes = [i64, i64, i64, vp, i64, vp, i64, i64, vp, i64, vp, i64, i64, vp, i32, i64, i32, vp]
+    lib.ds3_grouped_gemm_mxfp4.argtypes = [i32, vp, i64, i64, i64, vp, i64, vp, i64, i64, vp, i64, vp, i64, i64, vp, i32, i64, vp]
+    lib.ds3_moe_sort.argtypes = [vp, i64, i32, i64, i32, i32, vp, vp, vp]
+    lib.ds3_moe_dispatch.argtypes = [vp, i32, i64, i64, i64, vp, i32, i64, vp, i64, vp]
+    for name in ("ds3_moe_dispatch_quant_1x128", "ds3_moe_dispatch_quant_1x128_pow2", "ds3_moe_dispatch_quant_mxfp4"):
+        getattr(lib, name).argtypes = [vp, i32, i64, i64, i64, vp, i32, i64, vp, i64, vp, i64, i64, vp]
+    lib.ds3_moe_combine.argtypes = [vp, i32, i64, i64, i64, vp, vp, i64, i32, vp, i32, i64, vp]
+    lib.ds3_moe_combine_bwd.argtypes = [vp, i32, i64, vp, i32, i64, i64, i64, vp, vp, i64, i32, vp, i64, vp, vp]
     for name in SYMBOLS:
         getattr(lib, name)
     return lib
@@ -411,6 +425,82 @@ def ds3_retile_1x128_to_128x1(q: torch.Tensor, s: torch.Tensor, k_major_scales: 
 def ds3_retile_1x128_to_128x1_pow2(q: torch.Tensor, s: torch.Tensor, k_major_scales: bool = True):
     """As ds3_retile_1x128_to_128x1 with power-of-two output scales."""
     return (_native or _load_native()).retile(q, s, k_major_scales, True)
+
+
+def ds3_quant_mxfp4(x: torch.Tensor, k_major_scales: bool = True):
+    """x [M][K] FP32/BF16 -> MXFP4 in groups of 32 along K: (codes uint8 [M][K/2], two a byte, scale words int32 logical
+    [M][ceil(K/128)], the bytes of four groups each)."""
+    return (_native or _load_native()).quant_mxfp4(x, k_major_scales, False)
+
+
+def ds3_quant_mxfp4_t(x: torch.Tensor, k_major_scales: bool = True):
+    """x [T][C] -> MXFP4 in groups of 32 along T, transposed: (codes uint8 [C][ceil(T/2)], scale words logical [C][ceil(T/128)])."""
+    return (_native or _load_native()).quant_mxfp4(x, k_major_scales, True)
+
+
+def ds3_dequant_mxfp4(q: torch.Tensor, s: torch.Tensor, cols: int | None = None):
+    """MXFP4 codes and scale words -> BF16 [M][cols] (by default two columns for every byte of a row)."""
+    return (_native or _load_native()).dequant_mxfp4(q, s, -1 if cols is None else cols)
+
+
+def _is_f32(out_dtype) -> bool:
+    if out_dtype is not torch.bfloat16 and out_dtype is not torch.float32:
+        raise TypeError(f"unsupported dtype {out_dtype}")
+    return out_dtype is torch.float32
+
+
+def ds3_gemm_mxfp4(a, sa, b, sb, out_dtype=torch.bfloat16, c: torch.Tensor | None = None, accumulate: bool = False):
+    """C[M][N] (+)= product of MXFP4 codes a [M][K/2] (scale words sa, logical [M][K/128]) and b [N][K/2] (sb [N][K/128]);
+    K % 128 == 0.  c: the output (its type counts then); accumulate: FP32 only."""
+    return (_native or _load_native()).gemm_mxfp4(a, sa, b, sb, _is_f32(out_dtype), c, accumulate)
+
+
+def ds3_grouped_gemm_mxfp4(a, sa, group_offsets, b, sb, out_dtype=torch.bfloat16, c: torch.Tensor | None = None):
+    """Per expert g: rows [off[g], off[g+1]) of a times b[g] ([G][N][K/2] codes, scale words sb logical [G][N][K/128], one
+    expert's behind the other's).  Rows behind the last group are left as they were."""
+    return (_native or _load_native()).grouped_gemm_mxfp4(a, sa, group_offsets, b, sb, _is_f32(out_dtype), c)
+
+
+def ds3_moe_sort(expert_ids: torch.Tensor, num_experts: int, first_expert: int = 0):
+    """expert_ids int32 [T][top_k] (any number outside [first_expert, first_expert + num_experts): no row here) ->
+    (group_offsets int32 [num_experts + 1], row_of_slot int32 [T][top_k], -1 without a row), rows ordered by expert, token, slot."""
+    return (_native or _load_native()).moe_sort(expert_ids, num_experts, first_expert)
+
+
+def ds3_moe_dispatch(x: torch.Tensor, row_of_slot: torch.Tensor, rows: int | None = None, out: torch.Tensor | None = None):
+    """x [T][H] -> y [rows][H] with y[row_of_slot[t][j]] = x[t]; rows: by default one for every choice.  Choices whose row is
+    not below `rows` are dropped, rows that no choice names are left as they were."""
+    return (_native or _load_native()).moe_dispatch(x, row_of_slot, rows, out)
+
+
+def ds3_moe_dispatch_quant_1x128(x, row_of_slot, rows: int | None = None, out: tuple | None = None, k_major_scales: bool = True):
+    """As ds3_moe_dispatch with the 1x128 quantizer on the way: (codes [rows][H], scales logical [rows][ceil(H/128)])."""
+    return (_native or _load_native()).moe_dispatch_quant(x, row_of_slot, rows, out, k_major_scales, 0)
+
+
+def ds3_moe_dispatch_quant_1x128_pow2(x, row_of_slot, rows: int | None = None, out: tuple | None = None, k_major_scales: bool = True):
+    """As ds3_moe_dispatch_quant_1x128 with power-of-two scales."""
+    return (_native or _load_native()).moe_dispatch_quant(x, row_of_slot, rows, out, k_major_scales, 1)
+
+
+def ds3_moe_dispatch_quant_mxfp4(x, row_of_slot, rows: int | None = None, out: tuple | None = None, k_major_scales: bool = True):
+    """As ds3_moe_dispatch with the MXFP4 quantizer on the way: (codes [rows][H/2], scale words logical [rows][ceil(H/128)])."""
+    return (_native or _load_native()).moe_dispatch_quant(x, row_of_slot, rows, out, k_major_scales, 2)
+
+
+def ds3_moe_combine(y: torch.Tensor, row_of_slot: torch.Tensor, weights: torch.Tensor | None = None, out_dtype=None,
+                    out: torch.Tensor | None = None):
+    """out[t] = sum over j of weights[t][j] * y[row_of_slot[t][j]] in FP32 (weights None: ones, the gradient of the dispatch);
+    choices without a row add nothing.  out_dtype: by default y's."""
+    kind = 0 if out_dtype is None else 1 if _is_f32(out_dtype) else 2
+    return (_native or _load_native()).moe_combine(y, row_of_slot, weights, kind, out)
+
+
+def ds3_moe_combine_bwd(dout: torch.Tensor, y: torch.Tensor, row_of_slot: torch.Tensor, weights: torch.Tensor | None = None,
+                        dy: torch.Tensor | None = None):
+    """Gradients of ds3_moe_combine: (dy [rows][H] in y's type, dweights FP32 [T][top_k], 0 without a row).  Rows that no choice
+    names are left as they were (without `dy`: whatever the memory held)."""
+    return (_native or _load_native()).moe_combine_bwd(dout, y, row_of_slot, weights, dy)
 
 
 def ds3_gemm_num_variants() -> int:

@@ -516,6 +516,220 @@ ds3_status ds3_probe_lds_feed(const void* src, size_t window_bytes, int64_t row_
                              static_cast<hipStream_t>(stream));
 }
 
+// ---- MXFP4 -------------------------------------------------------------------------
+static bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+// Host-visible rules of a matrix in packed codes: `width` elements a row.
+static ds3_status check_mx_codes(const void* q, int64_t width, int64_t ldq, const void* s) {
+    if (ldq < (width + 1) / 2) return DS3_ERR_SHAPE;
+    if (!aligned16(q) || ldq % 16 || !aligned4(s)) return DS3_ERR_ALIGN;
+    return DS3_OK;
+}
+static ds3_status check_mx_source(const void* x, ds3_dtype xt, int64_t rows, int64_t cols, int64_t ldx) {
+    if (ldx < cols) return DS3_ERR_SHAPE;
+    if (rows > kMaxDim || cols > kMaxDim) return DS3_ERR_UNSUPPORTED;
+    const int64_t es = esize(xt);
+    if (!aligned16(x) || (ldx * es) % 16 || (cols * es) % 16) return DS3_ERR_ALIGN;
+    return DS3_OK;
+}
+
+static ds3_status quant_mx(bool transposed, const void* x, ds3_dtype xt, int64_t rows, int64_t cols, int64_t ldx, uint8_t* q,
+                           int64_t ldq, uint32_t* s, int64_t ss0, int64_t ss1, void* stream) {
+    if (!dtype_ok(xt)) return DS3_ERR_DTYPE;
+    if (rows < 0 || cols < 0) return DS3_ERR_SHAPE;
+    if (rows == 0 || cols == 0) return DS3_OK;
+    if (!x || !q || !s) return DS3_ERR_NULL;
+    ds3_status st = check_mx_source(x, xt, rows, cols, ldx);
+    if (st == DS3_OK) st = check_mx_codes(q, transposed ? rows : cols, ldq, s);
+    if (st != DS3_OK) return st;
+    return (transposed ? launch_quant_mxfp4_t : launch_quant_mxfp4)(x, xt, rows, cols, ldx, q, ldq, s, ss0, ss1, static_cast<hipStream_t>(stream));
+}
+ds3_status ds3_quant_mxfp4(const void* x, ds3_dtype xt, int64_t rows, int64_t cols, int64_t ldx, uint8_t* q, int64_t ldq,
+                           uint32_t* s, int64_t s_stride_row, int64_t s_stride_kb, void* stream) {
+    return quant_mx(false, x, xt, rows, cols, ldx, q, ldq, s, s_stride_row, s_stride_kb, stream);
+}
+ds3_status ds3_quant_mxfp4_t(const void* x, ds3_dtype xt, int64_t rows, int64_t cols, int64_t ldx, uint8_t* q_t, int64_t ldq,
+                             uint32_t* s_t, int64_t s_stride_col, int64_t s_stride_rb, void* stream) {
+    return quant_mx(true, x, xt, rows, cols, ldx, q_t, ldq, s_t, s_stride_col, s_stride_rb, stream);
+}
+
+ds3_status ds3_dequant_mxfp4(const uint8_t* q, int64_t rows, int64_t cols, int64_t ldq, const uint32_t* s, int64_t s_stride_row,
+                             int64_t s_stride_kb, void* y, int64_t ldy, void* stream) {
+    if (rows < 0 || cols < 0) return DS3_ERR_SHAPE;
+    if (rows == 0 || cols == 0) return DS3_OK;
+    if (!q || !s || !y) return DS3_ERR_NULL;
+    if (ldy < cols) return DS3_ERR_SHAPE;
+    if (rows > kMaxDim || cols > kMaxDim) return DS3_ERR_UNSUPPORTED;
+    if (!aligned16(y) || ldy % 8) return DS3_ERR_ALIGN;
+    const ds3_status st = check_mx_codes(q, cols, ldq, s);
+    if (st != DS3_OK) return st;
+    return launch_dequant_mxfp4(q, rows, cols, ldq, s, s_stride_row, s_stride_kb, y, ldy, static_cast<hipStream_t>(stream));
+}
+
+// The kernels address a matrix's scale words with byte offsets below 2^31 and non-negative strides.
+static bool scale_words_fit(int64_t rows, int64_t kw, int64_t sr, int64_t sk) {
+    const int64_t lim = (1ll << 29) - 1;
+    if (sr < 0 || sk < 0) return false;
+    if (rows - 1 > lim / (sr > 0 ? sr : 1) || kw - 1 > lim / (sk > 0 ? sk : 1)) return false;
+    return (rows - 1) * sr + (kw - 1) * sk <= lim;
+}
+
+static ds3_status gemm_mx(int32_t G, const int32_t* offs, int64_t M, int64_t N, int64_t K, const uint8_t* a, int64_t lda,
+                          const uint32_t* sa, int64_t sar, int64_t sak, const uint8_t* b, int64_t ldb, const uint32_t* sb,
+                          int64_t sbr, int64_t sbk, void* c, ds3_dtype ct, int64_t ldc, int accumulate, void* stream) {
+    if (!dtype_ok(ct)) return DS3_ERR_DTYPE;
+    if (accumulate && ct != DS3_F32) return DS3_ERR_DTYPE;
+    if (M < 0 || N < 0 || K < 0 || K % 128) return DS3_ERR_SHAPE;
+    if (M == 0 || N == 0) return DS3_OK;
+    if (!c) return DS3_ERR_NULL;
+    if (ldc < N) return DS3_ERR_SHAPE;
+    if (!aligned16(c) || ldc % 4) return DS3_ERR_ALIGN;
+    if (M > kMaxDim || N > kMaxDim || K > kMaxDim || G > 1023) return DS3_ERR_UNSUPPORTED;
+    if (K == 0)                                               // an empty sum: C += 0, or C = 0
+        return accumulate ? DS3_OK : G > 0 ? DS3_ERR_UNSUPPORTED : launch_zero_fill(c, ct, M, N, ldc, static_cast<hipStream_t>(stream));
+    if (!a || !b || !sa || !sb || (G > 0 && !offs)) return DS3_ERR_NULL;
+    if (lda < K / 2 || ldb < K / 2) return DS3_ERR_SHAPE;
+    if (!aligned16(a) || !aligned16(b) || lda % 16 || ldb % 16 || !aligned4(sa) || !aligned4(sb) || !aligned4(offs)) return DS3_ERR_ALIGN;
+    if (!scale_words_fit(M, K / 128, sar, sak) || !scale_words_fit(N, K / 128, sbr, sbk)) return DS3_ERR_UNSUPPORTED;
+    if (lda > kMaxDim || ldb > kMaxDim || (G > 0 && N > (1ll << 40) / ldb / G)) return DS3_ERR_UNSUPPORTED;
+    MxGemmParams p{};
+    p.a = a; p.b = b; p.sa = sa; p.sb = sb; p.c = c;
+    p.lda = lda; p.ldb = ldb; p.ldc = ldc;
+    p.sar = sar; p.sak = sak; p.sbr = sbr; p.sbk = sbk;
+    p.M = (int)M; p.N = (int)N; p.K = (int)K; p.G = G;
+    p.group_offsets = offs;
+    p.b_group_stride = N * ldb;
+    p.sb_group_stride = N * (K / 128);
+    p.accumulate = accumulate;
+    return launch_gemm_mxfp4(p, ct, static_cast<hipStream_t>(stream));
+}
+ds3_status ds3_gemm_mxfp4(int64_t M, int64_t N, int64_t K, const uint8_t* a, int64_t lda, const uint32_t* sa, int64_t sa_stride_row,
+                          int64_t sa_stride_kb, const uint8_t* b, int64_t ldb, const uint32_t* sb, int64_t sb_stride_row,
+                          int64_t sb_stride_kb, void* c, ds3_dtype ct, int64_t ldc, int accumulate, void* stream) {
+    return gemm_mx(0, nullptr, M, N, K, a, lda, sa, sa_stride_row, sa_stride_kb, b, ldb, sb, sb_stride_row, sb_stride_kb, c, ct, ldc,
+                   accumulate, stream);
+}
+ds3_status ds3_grouped_gemm_mxfp4(int32_t G, const int32_t* group_offsets, int64_t total_rows, int64_t N, int64_t K,
+                                  const uint8_t* a, int64_t lda, const uint32_t* sa, int64_t sa_stride_row, int64_t sa_stride_kb,
+                                  const uint8_t* b, int64_t ldb, const uint32_t* sb, int64_t sb_stride_row, int64_t sb_stride_kb,
+                                  void* c, ds3_dtype ct, int64_t ldc, void* stream) {
+    if (G < 0) return DS3_ERR_SHAPE;
+    if (G == 0) return DS3_OK;
+    return gemm_mx(G, group_offsets, total_rows, N, K, a, lda, sa, sa_stride_row, sa_stride_kb, b, ldb, sb, sb_stride_row, sb_stride_kb,
+                   c, ct, ldc, 0, stream);
+}
+
+// ---- rows in expert order and back ----------------------------------------------------
+constexpr int kMaxTopK = 64;                                  // one choice a lane
+static ds3_status check_slots(int64_t tokens, int64_t cols, int32_t top_k, int64_t total_rows) {
+    if (tokens < 0 || cols < 0 || top_k < 1 || total_rows < 0) return DS3_ERR_SHAPE;
+    if (top_k > kMaxTopK || tokens > kMaxDim / top_k || cols > kMaxDim || total_rows > kMaxDim) return DS3_ERR_UNSUPPORTED;
+    return DS3_OK;
+}
+
+ds3_status ds3_moe_sort(const int32_t* expert_ids, int64_t tokens, int32_t top_k, int64_t ld_ids, int32_t first_expert, int32_t G,
+                        int32_t* group_offsets, int32_t* row_of_slot, void* stream) {
+    const ds3_status st = check_slots(tokens, 0, top_k, 0);
+    if (st != DS3_OK) return st;
+    if (G < 0 || first_expert < 0 || ld_ids < top_k) return DS3_ERR_SHAPE;
+    if (G > 1023) return DS3_ERR_UNSUPPORTED;
+    if (!group_offsets || (tokens > 0 && (!expert_ids || !row_of_slot))) return DS3_ERR_NULL;
+    if (!aligned4(expert_ids) || !aligned4(group_offsets) || !aligned4(row_of_slot)) return DS3_ERR_ALIGN;
+    return launch_moe_sort(expert_ids, tokens, top_k, ld_ids, first_expert, G, group_offsets, row_of_slot, static_cast<hipStream_t>(stream));
+}
+
+static ds3_status dispatch(DispatchTo to, int pow2, const void* x, ds3_dtype xt, int64_t tokens, int64_t cols, int64_t ldx,
+                           const int32_t* row_of_slot, int32_t top_k, int64_t total_rows, void* y, int64_t ldy, void* s, int64_t ssr,
+                           int64_t ssk, void* stream) {
+    if (!dtype_ok(xt)) return DS3_ERR_DTYPE;
+    ds3_status st = check_slots(tokens, cols, top_k, total_rows);
+    if (st != DS3_OK) return st;
+    if (tokens == 0 || cols == 0 || total_rows == 0) return DS3_OK;
+    if (!x || !row_of_slot || !y || (to != kDispatchRows && !s)) return DS3_ERR_NULL;
+    const int64_t es = esize(xt), bytes = to == kDispatchRows ? es : 1;
+    if (ldx < cols || ldy < (to == kDispatchMx4 ? (cols + 1) / 2 : cols)) return DS3_ERR_SHAPE;
+    if (!aligned16(x) || !aligned16(y) || !aligned4(row_of_slot) || (to != kDispatchRows && !aligned4(s)) || (cols * es) % 16 ||
+        (ldx * es) % 16 || (ldy * bytes) % 16)
+        return DS3_ERR_ALIGN;
+    DispatchParams p{};
+    p.x = static_cast<const uint8_t*>(x);
+    p.tokens = tokens; p.cols = cols; p.ldx_bytes = ldx * es;
+    p.row_of_slot = row_of_slot; p.top_k = top_k; p.total_rows = total_rows;
+    p.y = static_cast<uint8_t*>(y);
+    p.ldy_bytes = ldy * bytes;
+    p.s = s; p.ssr = ssr; p.ssk = ssk; p.pow2 = pow2;
+    return launch_moe_dispatch(p, xt, to, static_cast<hipStream_t>(stream));
+}
+ds3_status ds3_moe_dispatch(const void* x, ds3_dtype xt, int64_t tokens, int64_t cols, int64_t ldx, const int32_t* row_of_slot,
+                            int32_t top_k, int64_t total_rows, void* y, int64_t ldy, void* stream) {
+    return dispatch(kDispatchRows, 0, x, xt, tokens, cols, ldx, row_of_slot, top_k, total_rows, y, ldy, nullptr, 0, 0, stream);
+}
+ds3_status ds3_moe_dispatch_quant_1x128(const void* x, ds3_dtype xt, int64_t tokens, int64_t cols, int64_t ldx,
+                                        const int32_t* row_of_slot, int32_t top_k, int64_t total_rows, uint8_t* q, int64_t ldq,
+                                        float* s, int64_t s_stride_row, int64_t s_stride_kb, void* stream) {
+    return dispatch(kDispatchFp8, 0, x, xt, tokens, cols, ldx, row_of_slot, top_k, total_rows, q, ldq, s, s_stride_row, s_stride_kb, stream);
+}
+ds3_status ds3_moe_dispatch_quant_1x128_pow2(const void* x, ds3_dtype xt, int64_t tokens, int64_t cols, int64_t ldx,
+                                             const int32_t* row_of_slot, int32_t top_k, int64_t total_rows, uint8_t* q, int64_t ldq,
+                                             float* s, int64_t s_stride_row, int64_t s_stride_kb, void* stream) {
+    return dispatch(kDispatchFp8, 1, x, xt, tokens, cols, ldx, row_of_slot, top_k, total_rows, q, ldq, s, s_stride_row, s_stride_kb, stream);
+}
+ds3_status ds3_moe_dispatch_quant_mxfp4(const void* x, ds3_dtype xt, int64_t tokens, int64_t cols, int64_t ldx,
+                                        const int32_t* row_of_slot, int32_t top_k, int64_t total_rows, uint8_t* q, int64_t ldq,
+                                        uint32_t* s, int64_t s_stride_row, int64_t s_stride_kb, void* stream) {
+    return dispatch(kDispatchMx4, 0, x, xt, tokens, cols, ldx, row_of_slot, top_k, total_rows, q, ldq, s, s_stride_row, s_stride_kb, stream);
+}
+
+// What both directions of combine ask of their matrices: y [total_rows][ldy] and the other [tokens][ldo].
+static ds3_status check_combine(const void* y, ds3_dtype yt, int64_t ldy, const void* o, ds3_dtype ot, int64_t ldo, int64_t cols,
+                                const int32_t* row_of_slot, const float* w) {
+    if (ldy < cols || ldo < cols) return DS3_ERR_SHAPE;
+    const int64_t ey = esize(yt), eo = esize(ot);
+    if (!aligned16(y) || !aligned16(o) || !aligned4(row_of_slot) || !aligned4(w) || (cols * ey) % 16 || (cols * eo) % 16 ||
+        (ldy * ey) % 16 || (ldo * eo) % 16)
+        return DS3_ERR_ALIGN;
+    return DS3_OK;
+}
+ds3_status ds3_moe_combine(const void* y, ds3_dtype yt, int64_t total_rows, int64_t cols, int64_t ldy, const int32_t* row_of_slot,
+                           const float* weights, int64_t tokens, int32_t top_k, void* out, ds3_dtype ot, int64_t ldo, void* stream) {
+    if (!dtype_ok(yt) || !dtype_ok(ot)) return DS3_ERR_DTYPE;
+    ds3_status st = check_slots(tokens, cols, top_k, total_rows);
+    if (st != DS3_OK) return st;
+    if (tokens == 0 || cols == 0) return DS3_OK;
+    if (!row_of_slot || !out || (total_rows > 0 && !y)) return DS3_ERR_NULL;
+    st = check_combine(y, yt, ldy, out, ot, ldo, cols, row_of_slot, weights);
+    if (st != DS3_OK) return st;
+    CombineParams p{};
+    p.y = static_cast<const uint8_t*>(y);
+    p.total_rows = total_rows; p.cols = cols; p.ldy_bytes = ldy * esize(yt);
+    p.row_of_slot = row_of_slot; p.w = weights; p.tokens = tokens; p.top_k = top_k;
+    p.out = static_cast<uint8_t*>(out);
+    p.ldo_bytes = ldo * esize(ot);
+    return launch_moe_combine(p, yt, ot, static_cast<hipStream_t>(stream));
+}
+ds3_status ds3_moe_combine_bwd(const void* dout, ds3_dtype ot, int64_t ldo, const void* y, ds3_dtype yt, int64_t total_rows,
+                               int64_t cols, int64_t ldy, const int32_t* row_of_slot, const float* weights, int64_t tokens,
+                               int32_t top_k, void* dy, int64_t lddy, float* dweights, void* stream) {
+    if (!dtype_ok(yt) || !dtype_ok(ot)) return DS3_ERR_DTYPE;
+    ds3_status st = check_slots(tokens, cols, top_k, total_rows);
+    if (st != DS3_OK) return st;
+    if (tokens == 0 || cols == 0) return DS3_OK;
+    if (!row_of_slot || !dout || !dweights || (total_rows > 0 && (!y || !dy))) return DS3_ERR_NULL;
+    st = check_combine(y, yt, ldy, dout, ot, ldo, cols, row_of_slot, weights);
+    if (st != DS3_OK) return st;
+    if (lddy < cols) return DS3_ERR_SHAPE;
+    if (!aligned16(dy) || (lddy * esize(yt)) % 16 || !aligned4(dweights)) return DS3_ERR_ALIGN;
+    CombineParams p{};
+    p.y = static_cast<const uint8_t*>(y);
+    p.total_rows = total_rows; p.cols = cols; p.ldy_bytes = ldy * esize(yt);
+    p.row_of_slot = row_of_slot; p.w = weights; p.tokens = tokens; p.top_k = top_k;
+    p.out = static_cast<uint8_t*>(const_cast<void*>(dout));
+    p.ldo_bytes = ldo * esize(ot);
+    p.dy = static_cast<uint8_t*>(dy);
+    p.lddy_bytes = lddy * esize(yt);
+    p.dw = dweights;
+    return launch_moe_combine_bwd(p, yt, ot, static_cast<hipStream_t>(stream));
+}
+
 const char* ds3_status_string(ds3_status st) {
     switch (st) {
         case DS3_OK: return "ok";

@@ -12,6 +12,7 @@
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
 #include <ATen/ops/empty_strided.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -327,10 +328,276 @@ PyObject* gemm(PyObject*, PyObject* const* o, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// ---- MXFP4, and rows in expert order and back ------------------------------------------
+// The calls below launch on the current device's current stream: their tensors have to be there.
+const at::Tensor& here(PyObject* o, const char* name) {
+    const at::Tensor& t = tensor(o);
+    if (!t.is_cuda() || t.get_device() != c10::hip::current_device()) {
+        PyErr_Format(PyExc_ValueError, "%s must be on the current device", name);
+        throw python_error();
+    }
+    return t;
+}
+// As rows2d; one without elements has no strides to speak of.
+Mat mat2d(const at::Tensor& t, const char* name) {
+    if (t.dim() == 2 && t.numel() == 0) return {t.size(0), t.size(1), t.size(1)};
+    return rows2d(t, name);
+}
+void need_type(const at::Tensor& t, at::ScalarType type, const char* text) {
+    if (t.scalar_type() != type) fail(PyExc_TypeError, text);
+}
+at::Tensor scale_words(int64_t rows, int64_t nb, bool k_major, const at::Tensor& like) {
+    const auto opt = at::TensorOptions().dtype(at::kInt).device(like.device());
+    return k_major ? at::empty_strided({rows, nb}, {1, std::max<int64_t>(rows, 1)}, opt) : at::empty({rows, nb}, opt);
+}
+// Scales of `rows` rows in blocks of 128 elements, logical [rows][nb] with any strides.
+void need_scales(const at::Tensor& s, at::ScalarType type, int64_t rows, int64_t nb, const char* text) {
+    if (s.scalar_type() != type || s.dim() != 2 || s.size(0) != rows || s.size(1) != nb) fail(PyExc_ValueError, text);
+}
+PyObject* again(PyObject* given, const at::Tensor& made) {
+    if (given == Py_None) return THPVariable_Wrap(made);
+    Py_INCREF(given);
+    return given;
+}
+
+// (x, k_major_scales, transposed) -> (packed codes, scale words)
+PyObject* quant_mxfp4(PyObject*, PyObject* const* o, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    need(n, 3);
+    const at::Tensor& x = here(o[0], "x");
+    const bool km = truth(o[1]), tr = truth(o[2]);
+    const Mat m = mat2d(x, "x");
+    const ds3_dtype t = dtype_of(x);
+    const int64_t rows = tr ? m.cols : m.rows, cols = tr ? m.rows : m.cols;
+    const at::Tensor q = codes(rows, (cols + 1) / 2, x), s = scale_words(rows, blocks(cols), km, x);
+    void* st = stream();
+    call(tr ? "ds3_quant_mxfp4_t" : "ds3_quant_mxfp4", tr ? ds3_quant_mxfp4_t : ds3_quant_mxfp4, ptr(x), t, m.rows, m.cols, m.ld,
+         ptr(q), up((cols + 1) / 2, 16), ptr<uint32_t>(s), s.stride(0), s.stride(1), st);
+    return pair(q, s);
+    END_HANDLE_TH_ERRORS
+}
+
+// (q, s, cols or -1) -> y BF16
+PyObject* dequant_mxfp4(PyObject*, PyObject* const* o, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    need(n, 3);
+    const at::Tensor &q = here(o[0], "q"), &s = here(o[1], "s");
+    const Mat m = mat2d(q, "q");
+    int64_t cols = integer(o[2]);
+    if (cols < 0) cols = 2 * m.cols;
+    need_type(q, at::kByte, "q must be uint8");
+    if ((cols + 1) / 2 != m.cols) fail(PyExc_ValueError, "q must hold two columns a byte");
+    need_scales(s, at::kInt, m.rows, blocks(cols), "s must be int32, logical [rows][ceil(cols / 128)]");
+    const at::Tensor y = gemm_out(m.rows, cols, at::kBFloat16, q);
+    void* st = stream();
+    call("ds3_dequant_mxfp4", ds3_dequant_mxfp4, ptr(q), m.rows, cols, m.ld, ptr<uint32_t>(s), s.stride(0), s.stride(1), y.data_ptr(),
+         up(cols, 8), st);
+    return THPVariable_Wrap(y);
+    END_HANDLE_TH_ERRORS
+}
+
+// (a, sa, b, sb, f32_out, c or None, accumulate) -> c
+PyObject* gemm_mxfp4(PyObject*, PyObject* const* o, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    need(n, 7);
+    const at::Tensor &a = here(o[0], "a"), &sa = here(o[1], "sa"), &b = here(o[2], "b"), &sb = here(o[3], "sb");
+    const bool f32 = truth(o[4]), acc = truth(o[6]);
+    const Mat ma = mat2d(a, "a"), mb = mat2d(b, "b");
+    need_type(a, at::kByte, "a must be uint8");
+    need_type(b, at::kByte, "b must be uint8");
+    if (ma.cols != mb.cols) fail(PyExc_ValueError, "a and b disagree on K");
+    const int64_t k = 2 * ma.cols;
+    need_scales(sa, at::kInt, ma.rows, blocks(k), "sa must be int32, logical [M][K / 128]");
+    need_scales(sb, at::kInt, mb.rows, blocks(k), "sb must be int32, logical [N][K / 128]");
+    const at::Tensor c = o[5] == Py_None ? gemm_out(ma.rows, mb.rows, f32 ? at::kFloat : at::kBFloat16, a) : here(o[5], "c");
+    const Mat mc = mat2d(c, "c");
+    if (mc.rows != ma.rows || mc.cols != mb.rows) fail(PyExc_ValueError, "c must be [M][N]");
+    if (o[5] == Py_None && acc) fail(PyExc_ValueError, "nothing to accumulate into");
+    const ds3_dtype ct = dtype_of(c);
+    void* st = stream();
+    call("ds3_gemm_mxfp4", ds3_gemm_mxfp4, ma.rows, mb.rows, k, ptr(a), ma.ld, ptr<uint32_t>(sa), sa.stride(0), sa.stride(1), ptr(b),
+         mb.ld, ptr<uint32_t>(sb), sb.stride(0), sb.stride(1), c.data_ptr(), ct, mc.ld, (int)acc, st);
+    return again(o[5], c);
+    END_HANDLE_TH_ERRORS
+}
+
+// (a, sa, group_offsets, b, sb, f32_out, c or None) -> c
+PyObject* grouped_gemm_mxfp4(PyObject*, PyObject* const* o, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    need(n, 7);
+    const at::Tensor &a = here(o[0], "a"), &sa = here(o[1], "sa"), &off = here(o[2], "group_offsets"), &b = here(o[3], "b"), &sb = here(o[4], "sb");
+    const bool f32 = truth(o[5]);
+    const Mat ma = mat2d(a, "a");
+    need_type(a, at::kByte, "a must be uint8");
+    need_type(b, at::kByte, "b must be uint8");
+    if (b.dim() != 3 || b.size(2) != ma.cols || !b.is_contiguous()) fail(PyExc_ValueError, "b must be contiguous [G][N][K / 2]");
+    const int64_t g = b.size(0), nn = b.size(1), k = 2 * ma.cols;
+    if (off.scalar_type() != at::kInt || off.dim() != 1 || off.size(0) != g + 1 || !off.is_contiguous())
+        fail(PyExc_ValueError, "group_offsets must be contiguous int32 of length G+1");
+    need_scales(sa, at::kInt, ma.rows, blocks(k), "sa must be int32, logical [rows][K / 128]");
+    if (sb.scalar_type() != at::kInt || sb.dim() != 3 || sb.size(0) != g || sb.size(1) != nn || sb.size(2) != blocks(k) ||
+        (g > 1 && sb.stride(0) != nn * blocks(k)))
+        fail(PyExc_ValueError, "sb must be int32, logical [G][N][K / 128], one expert's words behind the other's");
+    const at::Tensor c = o[6] == Py_None ? gemm_out(ma.rows, nn, f32 ? at::kFloat : at::kBFloat16, a) : here(o[6], "c");
+    const Mat mc = mat2d(c, "c");
+    if (mc.rows != ma.rows || mc.cols != nn) fail(PyExc_ValueError, "c must be [rows][N]");
+    const ds3_dtype ct = dtype_of(c);
+    if (g > INT32_MAX) fail(PyExc_ValueError, "too many experts");
+    void* st = stream();
+    call("ds3_grouped_gemm_mxfp4", ds3_grouped_gemm_mxfp4, (int32_t)g, ptr<int32_t>(off), ma.rows, nn, k, ptr(a), ma.ld, ptr<uint32_t>(sa),
+         sa.stride(0), sa.stride(1), ptr(b), ma.cols, ptr<uint32_t>(sb), sb.stride(1), sb.stride(2), c.data_ptr(), ct, mc.ld, st);
+    return again(o[6], c);
+    END_HANDLE_TH_ERRORS
+}
+
+// (expert_ids, G, first_expert) -> (group_offsets, row_of_slot)
+PyObject* moe_sort(PyObject*, PyObject* const* o, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    need(n, 3);
+    const at::Tensor& ids = here(o[0], "expert_ids");
+    const int64_t g = integer(o[1]), first = integer(o[2]);
+    need_type(ids, at::kInt, "expert_ids must be int32");
+    const Mat m = mat2d(ids, "expert_ids");
+    if (g < 0 || g > INT32_MAX || first < 0 || first > INT32_MAX || m.cols > INT32_MAX) fail(PyExc_ValueError, "bad number of experts");
+    const auto opt = at::TensorOptions().dtype(at::kInt).device(ids.device());
+    const at::Tensor off = at::empty({g + 1}, opt), rows = at::empty({m.rows, m.cols}, opt);
+    void* st = stream();
+    call("ds3_moe_sort", ds3_moe_sort, ptr<int32_t>(ids), m.rows, (int32_t)m.cols, m.ld, (int32_t)first, (int32_t)g, ptr<int32_t>(off),
+         ptr<int32_t>(rows), st);
+    return pair(off, rows);
+    END_HANDLE_TH_ERRORS
+}
+
+// row_of_slot [tokens][top_k], contiguous
+const at::Tensor& slots(PyObject* o) {
+    const at::Tensor& r = here(o, "row_of_slot");
+    if (r.scalar_type() != at::kInt || r.dim() != 2 || !r.is_contiguous() || r.size(1) > INT32_MAX)
+        fail(PyExc_ValueError, "row_of_slot must be contiguous int32 [tokens][top_k]");
+    return r;
+}
+int64_t rows_given(PyObject* o, const at::Tensor& r) {
+    return o == Py_None ? r.numel() : integer(o);
+}
+
+// (x, row_of_slot, rows or None, out or None) -> y
+PyObject* moe_dispatch(PyObject*, PyObject* const* o, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    need(n, 4);
+    const at::Tensor &x = here(o[0], "x"), &r = slots(o[1]);
+    const Mat m = mat2d(x, "x");
+    const ds3_dtype t = dtype_of(x);
+    if (r.size(0) != m.rows) fail(PyExc_ValueError, "x and row_of_slot disagree on the tokens");
+    const int64_t total = rows_given(o[2], r);
+    if (total < 0) fail(PyExc_ValueError, "rows must not be negative");
+    const at::Tensor y = o[3] == Py_None ? empty2d(total, m.cols, up(m.cols, 8), x.scalar_type(), x) : here(o[3], "out");
+    const Mat my = mat2d(y, "out");
+    if (y.scalar_type() != x.scalar_type() || my.cols != m.cols || (o[2] != Py_None && my.rows != total))
+        fail(PyExc_ValueError, "out must be [rows][columns of x] of x's type");
+    void* st = stream();
+    call("ds3_moe_dispatch", ds3_moe_dispatch, ptr(x), t, m.rows, m.cols, m.ld, ptr<int32_t>(r), (int32_t)r.size(1), my.rows, y.data_ptr(),
+         my.ld, st);
+    return again(o[3], y);
+    END_HANDLE_TH_ERRORS
+}
+
+// (x, row_of_slot, rows or None, out or None, k_major_scales, form) -> (codes, scales); form 0: 1x128, 1: its power-of-two
+// form, 2: MXFP4
+PyObject* moe_dispatch_quant(PyObject*, PyObject* const* o, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    need(n, 6);
+    const at::Tensor &x = here(o[0], "x"), &r = slots(o[1]);
+    const Mat m = mat2d(x, "x");
+    const ds3_dtype t = dtype_of(x);
+    const bool km = truth(o[4]);
+    const int64_t form = integer(o[5]);
+    if (r.size(0) != m.rows) fail(PyExc_ValueError, "x and row_of_slot disagree on the tokens");
+    const int64_t width = form == 2 ? (m.cols + 1) / 2 : m.cols, nb = blocks(m.cols);
+    const at::ScalarType stype = form == 2 ? at::kInt : at::kFloat;
+    int64_t total = rows_given(o[2], r);
+    if (total < 0) fail(PyExc_ValueError, "rows must not be negative");
+    at::Tensor q, s;
+    if (o[3] == Py_None) {
+        q = codes(total, width, x);
+        s = form == 2 ? scale_words(total, nb, km, x) : scales(total, nb, km, x);
+    } else {
+        if (!PyTuple_Check(o[3]) || PyTuple_GET_SIZE(o[3]) != 2) fail(PyExc_TypeError, "out must be a pair (codes, scales)");
+        q = here(PyTuple_GET_ITEM(o[3], 0), "out");
+        s = here(PyTuple_GET_ITEM(o[3], 1), "out");
+    }
+    const Mat mq = mat2d(q, "out");
+    if (q.scalar_type() != at::kByte || mq.cols != width || (o[2] != Py_None && mq.rows != total))
+        fail(PyExc_ValueError, "out's codes must be uint8 [rows][bytes of a row]");
+    need_scales(s, stype, mq.rows, nb, "out's scales must be logical [rows][ceil(columns / 128)], FP32 (MXFP4: int32)");
+    if (mq.rows > 1 && nb > 0 && (s.stride(0) == 0 || (nb > 1 && s.stride(1) == 0))) fail(PyExc_ValueError, "out's scales overlap");
+    void* st = stream();
+    if (form == 2)
+        call("ds3_moe_dispatch_quant_mxfp4", ds3_moe_dispatch_quant_mxfp4, ptr(x), t, m.rows, m.cols, m.ld, ptr<int32_t>(r),
+             (int32_t)r.size(1), mq.rows, ptr(q), mq.ld, ptr<uint32_t>(s), s.stride(0), s.stride(1), st);
+    else
+        call(form ? "ds3_moe_dispatch_quant_1x128_pow2" : "ds3_moe_dispatch_quant_1x128",
+             form ? ds3_moe_dispatch_quant_1x128_pow2 : ds3_moe_dispatch_quant_1x128, ptr(x), t, m.rows, m.cols, m.ld, ptr<int32_t>(r),
+             (int32_t)r.size(1), mq.rows, ptr(q), mq.ld, ptr<float>(s), s.stride(0), s.stride(1), st);
+    if (o[3] == Py_None) return pair(q, s);
+    Py_INCREF(o[3]);
+    return o[3];
+    END_HANDLE_TH_ERRORS
+}
+
+// weights [tokens][top_k] FP32 contiguous, or None
+const float* weights_of(PyObject* o, const at::Tensor& r) {
+    if (o == Py_None) return nullptr;
+    const at::Tensor& w = here(o, "weights");
+    if (w.scalar_type() != at::kFloat || !w.is_contiguous() || !w.sizes().equals(r.sizes()))
+        fail(PyExc_ValueError, "weights must be contiguous FP32 [tokens][top_k]");
+    return ptr<float>(w);
+}
+
+// (y, row_of_slot, weights or None, out type: 0 as y, 1 FP32, 2 BF16, out or None) -> out
+PyObject* moe_combine(PyObject*, PyObject* const* o, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    need(n, 5);
+    const at::Tensor &y = here(o[0], "y"), &r = slots(o[1]);
+    const Mat m = mat2d(y, "y");
+    const ds3_dtype yt = dtype_of(y);
+    const float* w = weights_of(o[2], r);
+    const int64_t type = integer(o[3]);
+    const at::ScalarType otype = type == 1 ? at::kFloat : type == 2 ? at::kBFloat16 : y.scalar_type();
+    const at::Tensor out = o[4] == Py_None ? empty2d(r.size(0), m.cols, up(m.cols, 8), otype, y) : here(o[4], "out");
+    const Mat mo = mat2d(out, "out");
+    const ds3_dtype ot = dtype_of(out);
+    if (mo.rows != r.size(0) || mo.cols != m.cols) fail(PyExc_ValueError, "out must be [tokens][columns of y]");
+    void* st = stream();
+    call("ds3_moe_combine", ds3_moe_combine, y.data_ptr(), yt, m.rows, m.cols, m.ld, ptr<int32_t>(r), w, r.size(0), (int32_t)r.size(1),
+         out.data_ptr(), ot, mo.ld, st);
+    return again(o[4], out);
+    END_HANDLE_TH_ERRORS
+}
+
+// (dout, y, row_of_slot, weights or None, dy or None) -> (dy, dweights)
+PyObject* moe_combine_bwd(PyObject*, PyObject* const* o, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    need(n, 5);
+    const at::Tensor &d = here(o[0], "dout"), &y = here(o[1], "y"), &r = slots(o[2]);
+    const Mat md = mat2d(d, "dout"), m = mat2d(y, "y");
+    const ds3_dtype ot = dtype_of(d), yt = dtype_of(y);
+    const float* w = weights_of(o[3], r);
+    if (md.rows != r.size(0) || md.cols != m.cols) fail(PyExc_ValueError, "dout must be [tokens][columns of y]");
+    const at::Tensor dy = o[4] == Py_None ? empty2d(m.rows, m.cols, up(m.cols, 8), y.scalar_type(), y) : here(o[4], "dy");
+    const Mat my = mat2d(dy, "dy");
+    if (dy.scalar_type() != y.scalar_type() || my.rows != m.rows || my.cols != m.cols) fail(PyExc_ValueError, "dy must be as y");
+    const at::Tensor dw = at::empty({r.size(0), r.size(1)}, at::TensorOptions().dtype(at::kFloat).device(y.device()));
+    void* st = stream();
+    call("ds3_moe_combine_bwd", ds3_moe_combine_bwd, d.data_ptr(), ot, md.ld, y.data_ptr(), yt, m.rows, m.cols, m.ld, ptr<int32_t>(r), w,
+         r.size(0), (int32_t)r.size(1), dy.data_ptr(), my.ld, ptr<float>(dw), st);
+    return pair(dy, dw);
+    END_HANDLE_TH_ERRORS
+}
+
 PyMethodDef kMethods[] = {
 #define M(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
     M(quant_act_1x128), M(quant_act_128x1), M(quant_w_128x128), M(quant_w_128x128_dual), M(swiglu_quant_1x128), M(rmsnorm_quant_1x128), M(retile),
-    M(quant_act_1x128_e5m6), M(gemm),
+    M(quant_act_1x128_e5m6), M(gemm), M(quant_mxfp4), M(dequant_mxfp4), M(gemm_mxfp4), M(grouped_gemm_mxfp4),
+    M(moe_sort), M(moe_dispatch), M(moe_dispatch_quant), M(moe_combine), M(moe_combine_bwd),
 #undef M
     {"init", [](PyObject*, PyObject* args) -> PyObject* {
          PyObject *check, *kept, *make;

@@ -109,4 +109,65 @@ ds3_status launch_workspace_init(void* ws, size_t ws_bytes, hipStream_t st);
 // C[M][N] = 0 (the product over an empty inner dimension).
 ds3_status launch_zero_fill(void* c, ds3_dtype ct, int64_t M, int64_t N, int64_t ldc, hipStream_t st);
 
+// ---- MXFP4 -------------------------------------------------------------------------
+ds3_status launch_quant_mxfp4(const void* x, ds3_dtype xt, int64_t rows, int64_t cols, int64_t ldx, uint8_t* q, int64_t ldq,
+                              uint32_t* s, int64_t ssr, int64_t ssk, hipStream_t st);
+ds3_status launch_quant_mxfp4_t(const void* x, ds3_dtype xt, int64_t rows, int64_t cols, int64_t ldx, uint8_t* qt, int64_t ldq,
+                                uint32_t* s_t, int64_t ssc, int64_t sst, hipStream_t st);
+ds3_status launch_dequant_mxfp4(const uint8_t* q, int64_t rows, int64_t cols, int64_t ldq, const uint32_t* s, int64_t ssr,
+                                int64_t ssk, void* y, int64_t ldy, hipStream_t st);
+
+// One description for the dense (G == 0) and the grouped MXFP4 GEMM.
+struct MxGemmParams {
+    const uint8_t* a;         // [M][lda] packed codes
+    const uint8_t* b;         // [N][ldb] (grouped: [G][N][ldb])
+    const uint32_t* sa;       // scale words of 128 elements
+    const uint32_t* sb;
+    void* c;
+    int64_t lda, ldb, ldc;    // lda, ldb in bytes
+    int64_t sar, sak, sbr, sbk;   // strides in words: row, 128-element block
+    int64_t b_group_stride;   // bytes between experts in b
+    int64_t sb_group_stride;  // words between experts in sb
+    const int32_t* group_offsets;
+    int M, N, K;              // grouped: M = total rows
+    int G;
+    int tiles_m, tiles_n;
+    int accumulate;
+};
+ds3_status launch_gemm_mxfp4(const MxGemmParams& p, ds3_dtype ct, hipStream_t st);
+
+// ---- rows in expert order and back ----------------------------------------------------
+ds3_status launch_moe_sort(const int32_t* ids, int64_t tokens, int top_k, int64_t ld, int first, int G, int32_t* offsets,
+                           int32_t* row_of_slot, hipStream_t st);
+// What a dispatch leaves of a token's row.
+enum DispatchTo { kDispatchRows, kDispatchFp8, kDispatchMx4 };
+struct DispatchParams {
+    const uint8_t* x;
+    int64_t tokens, cols, ldx_bytes;
+    const int32_t* row_of_slot;
+    int top_k;
+    int64_t total_rows;
+    uint8_t* y;               // rows, or codes
+    int64_t ldy_bytes;
+    void* s;                  // scales (FP8), scale words (MXFP4)
+    int64_t ssr, ssk;
+    int pow2;
+};
+ds3_status launch_moe_dispatch(const DispatchParams& p, ds3_dtype xt, DispatchTo to, hipStream_t st);
+struct CombineParams {
+    const uint8_t* y;
+    int64_t total_rows, cols, ldy_bytes;
+    const int32_t* row_of_slot;
+    const float* w;           // [tokens][top_k] or nullptr: ones
+    int64_t tokens;
+    int top_k;
+    uint8_t* out;             // forward: the sums; backward: their gradient (read)
+    int64_t ldo_bytes;
+    uint8_t* dy;              // backward only
+    int64_t lddy_bytes;
+    float* dw;
+};
+ds3_status launch_moe_combine(const CombineParams& p, ds3_dtype yt, ds3_dtype ot, hipStream_t st);
+ds3_status launch_moe_combine_bwd(const CombineParams& p, ds3_dtype yt, ds3_dtype ot, hipStream_t st);
+
 }  // namespace ds3

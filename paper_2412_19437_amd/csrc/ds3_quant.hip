@@ -10,68 +10,6 @@
 
 namespace ds3 {
 
-// The quantizers touch every byte once: loads and stores carry the non-temporal hint
-// so that the streams do not displace each other in the L2 / last-level cache
-// (measured on MI355X: 6.2 TB/s instead of 5.5 TB/s for a 2:1 read:write stream).
-__device__ __forceinline__ u32x4 ld_stream(const uint8_t* p) {
-    return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
-}
-template <typename V>
-__device__ __forceinline__ void st_stream(uint8_t* p, V v) {
-    *reinterpret_cast<V*>(p) = v;
-}
-// Non-temporal store: for what is not read again soon (the optimizer step's states and weights,
-// 617 us a step where plain stores of the new weights take 633).  Codes are: the GEMM behind a fused
-// producer finds them in the memory-side cache where they went there by plain stores (8192 x 7168
-// behind RMSNorm, N 576: the GEMM 56 -> 42 us, the producer's time the same; SwiGLU and a 4096 x 7168 x
-// 18432 power-of-two product 484 -> 477 us.  Behind SwiGLU it is a small thing: the producer alone takes
-// .96 to 1.05 of its time with plain stores, it and the GEMM .975 to 1.02, 14 shapes, mean .999).  The plain
-// quantizers and the transposing kernels are 5-15% slower with non-temporal stores.
-template <typename V>
-__device__ __forceinline__ void st_nt(uint8_t* p, V v) {
-    __builtin_nontemporal_store(v, reinterpret_cast<V*>(p));
-}
-
-// Byte offset inside a [128 rows][128 + 16 bytes] LDS tile whose 16-byte chunks are
-// XOR-swizzled by a key taken from the row index (bits KS .. KS+2): the lanes of a
-// wave that write the same chunk position of rows 2^KS apart then hit different banks
-// (the row stride of 144 bytes alone repeats the bank every 16 rows).  `off` is the
-// byte offset inside the row; accesses never straddle a 16-byte chunk.
-template <int KS>
-__device__ __forceinline__ int tile_off(int row, int off) {
-    return row * 144 + ((((off >> 4) ^ (row >> KS)) & 7) << 4) + (off & 15);
-}
-
-// ----- element traits: how many elements one 16-byte load carries --------------
-struct Bf16 { static constexpr int EPL = 8; };   // elements per 128-bit load
-struct F32  { static constexpr int EPL = 4; };
-
-// Widen the EPL elements of one 16-byte granule to FP32.
-template <typename T> __device__ __forceinline__ void widen(const u32x4& g, float* v);
-template <> __device__ __forceinline__ void widen<Bf16>(const u32x4& g, float* v) {
-    v[0] = bf16_lo(g.x); v[1] = bf16_hi(g.x); v[2] = bf16_lo(g.y); v[3] = bf16_hi(g.y);
-    v[4] = bf16_lo(g.z); v[5] = bf16_hi(g.z); v[6] = bf16_lo(g.w); v[7] = bf16_hi(g.w);
-}
-template <> __device__ __forceinline__ void widen<F32>(const u32x4& g, float* v) {
-    v[0] = as_f32(g.x); v[1] = as_f32(g.y); v[2] = as_f32(g.z); v[3] = as_f32(g.w);
-}
-
-// max |element| of one granule, as the bit pattern of a non-negative float.
-template <typename T> __device__ __forceinline__ unsigned int granule_amax_bits(const u32x4& g);
-template <> __device__ __forceinline__ unsigned int granule_amax_bits<Bf16>(const u32x4& g) {
-    unsigned int m = 0;
-    const unsigned int w[4] = {g.x, g.y, g.z, g.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        m = umax(m, w[i] & 0x7fff0000u);
-        m = umax(m, (w[i] << 16) & 0x7fff0000u);
-    }
-    return m;
-}
-template <> __device__ __forceinline__ unsigned int granule_amax_bits<F32>(const u32x4& g) {
-    return umax(umax(g.x & 0x7fffffffu, g.y & 0x7fffffffu), umax(g.z & 0x7fffffffu, g.w & 0x7fffffffu));
-}
-
 // =============================================================================
 // 1x128: one 16-lane DPP row per tile.  A workgroup is 16 rows of the matrix
 // (one per DPP row of its 4 waves) by TPG consecutive tiles, so each lane has
