@@ -10,11 +10,14 @@
 // chunks 2 * g4 and 2 * g4 + 1, the groups of the same numbers, and the two matrix instructions take one of them each.
 // Both groups' scale bytes are then neighbours, one 16-bit LDS read, and the instruction's operand select picks the byte.
 #include <algorithm>
+#include <type_traits>
 
 #include "ds3_internal.h"
 #include "ds3_mx4_dev.h"
 
 namespace ds3 {
+
+constexpr int kMaxExperts = 1023;
 
 __device__ __forceinline__ f32x4 mfma_mx4(const i32x4& a, const i32x4& b, const f32x4& c, int sa, int sb, int half) {
     const i32x8 a8 = {a.x, a.y, a.z, a.w, 0, 0, 0, 0}, b8 = {b.x, b.y, b.z, b.w, 0, 0, 0, 0};
@@ -260,6 +263,414 @@ __global__ __launch_bounds__(C::NT) void gemm_mxfp4_tile_kernel(const MxGemmPara
     }
 }
 
+// ---- the kernel for many tiles ------------------------------------------------------
+// BN x BM output tiles, WN x WM waves, NS stages of LDS with loads NS - 1 K-steps ahead of the matrix instructions.
+template <int BN_, int BM_, int WN_, int WM_, int NS_>
+struct MainCfg {
+    static constexpr int BN = BN_, BM = BM_, WN = WN_, WM = WM_, NS = NS_;
+    static constexpr int NT = 64 * WN * WM;
+    static constexpr int TN = BN / WN, TM = BM / WM;   // wave tile
+    static constexpr int FN = TN / 16, FM = TM / 16, NSUB = FN * FM;
+    static constexpr int ROWS = BN + BM;
+    static constexpr int STAGE = ROWS * 128;           // bytes of codes per K-step
+    static constexpr int RPI = NT / 8;                 // tile rows one load instruction of the workgroup covers
+    static constexpr int LPT = ROWS / RPI;             // 16-byte loads per thread per K-step
+    static constexpr int TAILN = LPT < FN ? LPT : FN;  // of them issued right behind the barrier that frees their stage
+    static constexpr int HEADN = LPT - TAILN;          // and at the head of the next K-step
+    static constexpr int SROW = ROWS + 16;             // words between the two words of a row's scales (other banks)
+    static constexpr int SSTAGE = 2 * SROW * 4;        // bytes of scales per K-step
+    static constexpr int LDS_BYTES = NS * (STAGE + SSTAGE) + (kMaxExperts + 1) * 4;
+    static constexpr int WG_PER_CU = NT > 256 || LDS_BYTES > 80 * 1024 ? 1 : 2;
+    static_assert(BN % RPI == 0 && BM % RPI == 0 && RPI % 16 == 0, "load mapping");
+    static constexpr int SR = (ROWS + NT - 1) / NT;    // rows of scales a thread fetches
+    static_assert(BN % 64 == 0 && BM % 64 == 0, "a wave fetches scales of one side");
+    static_assert(SR == 1 || (SR == 2 && BN == NT && BM == NT), "one row of scales a thread, or one of each side");
+    static_assert(FM % 2 == 0 && HEADN <= NSUB - FN && LPT <= 2 * FN, "loads are interleaved with the matrix instructions");
+    static_assert((NT / 64) * 16 * (TN * 4 + 16) <= STAGE, "epilogue strips take the last stage");
+    static_assert(LDS_BYTES <= 160 * 1024, "LDS");
+};
+
+struct MxTile {
+    int m0, n0, m_rows, n_rows;
+    __amdgpu_buffer_rsrc_t rs_a, rs_b, rs_s[2];
+    unsigned s_off[2];         // byte offsets of the rows of scales this thread fetches from
+};
+
+// Persistent workgroups; XCD x (workgroups are dealt to the eight of them in turn) walks its eighth of the tile list.  The
+// K-step's order of instructions is pinned: the matrix instructions of all sub-tiles but the last activation fragment's,
+// ONE barrier (the next stage is complete, this one is read), then behind it the loads that refill this stage and the
+// next K-step's first fragments, under the last fragment's matrix instructions.
+template <class C, bool OUT_BF16, bool GROUPED>
+__global__ __launch_bounds__(C::NT) void gemm_mxfp4_kernel(const MxGemmParams p) {
+    constexpr int BN = C::BN, BM = C::BM, NT = C::NT, NS = C::NS, FN = C::FN, FM = C::FM, STAGE = C::STAGE, NSUB = C::NSUB;
+    __shared__ __attribute__((aligned(1024))) uint8_t smem[C::LDS_BYTES];
+    uint8_t* const scales = smem + NS * STAGE;
+    int* const before = reinterpret_cast<int*>(scales + NS * C::SSTAGE);       // [G + 1] row tiles before expert g
+
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wn = wave % C::WN, wm = wave / C::WN;
+    const int l16 = lane & 15, g4 = lane >> 4;
+    const int KW = p.K >> 7, KB = (KW + 1) >> 1;       // scale words a row; K-steps (the last may be half)
+
+    // ---- tile walk -------------------------------------------------------------------
+    int tiles_m = p.tiles_m;
+    if constexpr (GROUPED) {
+        auto row_of = [&](int g) { return max(0, min(p.group_offsets[g], p.M)); };
+        if (wave == 0) {
+            int cum = 0;
+            for (int g0 = 0; g0 < p.G; g0 += 64) {
+                const int g = g0 + lane;
+                int sum = g < p.G ? max(0, row_of(g + 1) - row_of(g) + BM - 1) / BM : 0;
+                const int mine = sum;
+#pragma unroll
+                for (int d = 1; d < 64; d <<= 1) {
+                    const int o = __shfl_up(sum, d);
+                    if (lane >= d) sum += o;
+                }
+                if (g < p.G) before[g] = cum + sum - mine;
+                cum += __builtin_amdgcn_readlane(sum, 63);
+            }
+            if (lane == 0) before[p.G] = cum;
+        }
+        __syncthreads();
+        tiles_m = before[p.G];
+    }
+    const int ntiles = tiles_m * p.tiles_n;
+    const int per_xcd = (ntiles + 7) >> 3;
+    const int xcd = (int)(blockIdx.x & 7), slot = (int)(blockIdx.x >> 3), nslots = (int)(gridDim.x >> 3);
+    const int mine = max(0, min(per_xcd, ntiles - xcd * per_xcd));     // tiles of this XCD
+    const int rounds = mine / nslots, tail = mine - rounds * nslots;
+    // What is left after the last full round: at most half as many tiles as workgroups are cut into halves of BM / 2
+    // rows, whose other half's waves issue no matrix instruction (a half takes .55 of a tile's time).
+    const bool halves = !GROUPED && C::WM == 2 && rounds > 0 && tail > 0 && 2 * tail <= nslots && p.M % BM == 0;
+    const int units = rounds + (halves ? (slot < 2 * tail ? 1 : 0) : (slot < tail ? 1 : 0));
+
+    const int kbytes = p.K >> 1;
+    auto setup = [&](int u, MxTile& c) -> bool {
+        if (u >= units) return false;
+        int local = u * nslots + slot, half = -1;
+        if (halves && u == rounds) { half = slot & 1; local = rounds * nslots + (slot >> 1); }
+        const int t = xcd * per_xcd + local;
+        int m0, m_end, n0, grp = 0;
+        if constexpr (!GROUPED) {
+            constexpr int PM = 4;                      // row tiles of a panel: the tiles side by side share operands
+            const int panel = PM * p.tiles_n;
+            const int pi = t / panel, r = t - pi * panel;
+            const int pm = min(PM, tiles_m - pi * PM);
+            m0 = (pi * PM + r % pm) * BM;
+            n0 = (r / pm) * BN;
+            m_end = p.M;
+            if (half >= 0) { m0 += half * (BM / 2); m_end = min(m_end, m0 + BM / 2); }
+        } else {
+            // expert by expert, then by column tile, the expert's row tiles innermost: side by side they share weights
+            int lo = 0, hi = p.G;                      // largest g with before[g] * tiles_n <= t
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (before[mid] * p.tiles_n <= t) lo = mid; else hi = mid;
+            }
+            grp = lo;
+            const int nt_g = before[grp + 1] - before[grp];
+            const int r = t - before[grp] * p.tiles_n;
+            n0 = (r / nt_g) * BN;
+            m0 = max(0, min(p.group_offsets[grp], p.M)) + (r % nt_g) * BM;
+            m_end = max(0, min(p.group_offsets[grp + 1], p.M));
+            // uniform, but read through vector registers: said so here, the descriptors live in scalar registers
+            grp = __builtin_amdgcn_readfirstlane(grp);
+            n0 = __builtin_amdgcn_readfirstlane(n0);
+            m0 = __builtin_amdgcn_readfirstlane(m0);
+            m_end = __builtin_amdgcn_readfirstlane(m_end);
+        }
+        c.m0 = m0; c.n0 = n0;
+        c.m_rows = min(m_end - m0, BM);
+        c.n_rows = min(p.N - n0, BN);
+        // Descriptors over the tile's valid bytes: rows beyond them read as zero and touch no memory.
+        c.rs_a = __builtin_amdgcn_make_buffer_rsrc((void*)(p.a + (int64_t)m0 * p.lda), 0, (int)((int64_t)(c.m_rows - 1) * p.lda + kbytes), 0x00020000);
+        c.rs_b = __builtin_amdgcn_make_buffer_rsrc((void*)(p.b + (int64_t)grp * p.b_group_stride + (int64_t)n0 * p.ldb), 0,
+                                                   (int)((int64_t)(c.n_rows - 1) * p.ldb + kbytes), 0x00020000);
+        // Thread t fetches the scales of tile row t (weight rows first) and, where there are more rows than threads, of
+        // row t + NT (rows past the valid ones repeat the last; all offsets are valid, the range check is not relied on).
+#pragma unroll
+        for (int r = 0; r < C::SR; ++r) {
+            const bool w_side = r * NT + wave * 64 < BN;
+            const int row = r * NT + tid;
+            c.rs_s[r] = __builtin_amdgcn_make_buffer_rsrc((void*)(w_side ? p.sb + (int64_t)grp * p.sb_group_stride : p.sa), 0, 0x7ffffffc, 0x00020000);
+            c.s_off[r] = w_side ? (unsigned)(n0 + min(row, c.n_rows - 1)) * (unsigned)p.sbr * 4u
+                                : (unsigned)(m0 + min(max(row - BN, 0), c.m_rows - 1)) * (unsigned)p.sar * 4u;
+        }
+        return true;
+    };
+
+    // this thread moves chunk position (tid & 7) of tile row i * RPI + (tid >> 3); 16-byte chunks are XOR-swizzled by row
+    const int lrow = tid >> 3;
+    const int gchunk = (tid & 7) ^ swz_key(lrow);
+    const unsigned voff_b = (unsigned)(lrow * (int)p.ldb + gchunk * 16), voff_a = (unsigned)(lrow * (int)p.lda + gchunk * 16);
+    const unsigned step_b = (unsigned)(C::RPI * (int)p.ldb), step_a = (unsigned)(C::RPI * (int)p.lda);
+    // a half K-step's second half: neither operand's codes are read there (zeros), the scales are the first half's again
+    const unsigned past_half = (KW & 1) && gchunk >= 4 ? kOobOffset : 0u;
+    const int key = swz_key(l16);
+    const int foff0 = l16 * 128 + (((2 * g4) ^ key) << 4), foff1 = l16 * 128 + (((2 * g4 + 1) ^ key) << 4);
+    const int p_base = wn * C::TN * 128, q_base = (BN + wm * C::TM) * 128;
+    // this lane's two scale bytes: word g4 / 2 of its row, bytes 2 * (g4 % 2) and the next
+    const int so = (g4 >> 1) * (C::SROW * 4) + (g4 & 1) * 2 + l16 * 4;
+    const int ps_base = so + wn * C::TN * 4, qs_base = so + (BN + wm * C::TM) * 4;
+    const bool scale_role = C::SR == 2 || wave * 64 < C::ROWS;
+    // (in vector registers: as scalars they would be re-read from the kernel arguments inside the K-loop)
+    unsigned sc_kstride[2] = {(unsigned)(wave * 64 < BN ? (int)p.sbk : (int)p.sak) * 4u, (unsigned)(int)p.sak * 4u};
+    asm volatile("" : "+v"(sc_kstride[0]), "+v"(sc_kstride[1]));
+
+    // byte offset of K-step kb for this thread's loads (out of range beyond the last)
+    auto koff_of = [&](int kb) -> unsigned {
+        const unsigned o = kb < KB ? (unsigned)kb << 7 : kOobOffset;
+        return kb == KB - 1 ? o | past_half : o;
+    };
+    auto issue_load = [&](const MxTile& c, int i, int stage, unsigned koff) {
+        const bool is_b = i * C::RPI < BN;
+        const int ii = is_b ? i : i - BN / C::RPI;
+        unsigned uoff = (unsigned)ii * (is_b ? step_b : step_a);
+        asm volatile("" : "+s"(uoff));                 // (summed in a scalar register, added last)
+        const unsigned voff = (is_b ? voff_b : voff_a) + uoff + koff;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(is_b ? c.rs_b : c.rs_a, (lds_ptr_t)(smem + stage * STAGE + (i * NT + wave * 64) * 16), 16,
+                                                 (int)voff, 0, 0, 0);
+    };
+    auto issue_scales = [&](const MxTile& c, int kb, int stage) {
+        if (!scale_role) return;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const unsigned kw = (unsigned)min(2 * kb + h, KW - 1);
+#pragma unroll
+            for (int r = 0; r < C::SR; ++r)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(c.rs_s[r], (lds_ptr_t)(scales + stage * C::SSTAGE + (h * C::SROW + r * NT + wave * 64) * 4), 4,
+                                                         (int)(c.s_off[r] + kw * sc_kstride[r]), 0, 0, 0);
+        }
+    };
+    struct Frag { i32x4 h0, h1; };
+    auto load_frag = [&](const uint8_t* base) -> Frag {
+        return Frag{*reinterpret_cast<const i32x4*>(base + foff0), *reinterpret_cast<const i32x4*>(base + foff1)};
+    };
+    auto read_scale = [&](int stage, int at) -> int { return *reinterpret_cast<const uint16_t*>(scales + stage * C::SSTAGE + at); };
+    // Barrier that lets the newest `keep` vector-memory operations of this wave stay in flight.
+    auto barrier_keep = [&](auto keep_tag) {
+        constexpr int keep = decltype(keep_tag)::value;
+        static_assert(keep >= 0 && keep < 16, "vmcnt immediate");
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(keep | 0x70);       // vmcnt(keep) lgkmcnt(0)
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    auto kstep_barrier = [&]() {
+        if constexpr (NS == 2) barrier_keep(std::integral_constant<int, 0>{});
+        else if (scale_role) barrier_keep(std::integral_constant<int, C::LPT + 2 * C::SR>{});
+        else barrier_keep(std::integral_constant<int, C::LPT>{});
+    };
+    auto issue_first_steps = [&](const MxTile& c) {
+#pragma unroll
+        for (int ks = 0; ks < NS - 1; ++ks) {
+            const unsigned koff = koff_of(ks);
+#pragma unroll
+            for (int i = 0; i < C::LPT; ++i) issue_load(c, i, ks, koff);
+            issue_scales(c, ks, ks);
+        }
+    };
+
+    MxTile cur;
+    int unit = 0;
+    if (!setup(unit, cur)) return;
+    issue_first_steps(cur);
+    for (;;) {
+        // ---- K-steps 0 .. NS-2 of `cur` are in flight into stages 0 .. NS-2 ----
+        __builtin_amdgcn_s_waitcnt(0x70);
+        __syncthreads();
+        {
+            const unsigned koff = koff_of(NS - 1);
+#pragma unroll
+            for (int i = 0; i < C::TAILN; ++i) issue_load(cur, i, NS - 1, koff);
+            issue_scales(cur, NS - 1, NS - 1);
+        }
+        Frag pf[FN], qf[2];
+        int ps[FN], qs[2];
+#pragma unroll
+        for (int i = 0; i < FN; ++i) {
+            pf[i] = load_frag(smem + p_base + i * 2048);
+            ps[i] = read_scale(0, ps_base + i * 64);
+        }
+        qf[0] = load_frag(smem + q_base);
+        qs[0] = read_scale(0, qs_base);
+        f32x4 acc[FN][FM];
+#pragma unroll
+        for (int i = 0; i < FN; ++i)
+#pragma unroll
+            for (int j = 0; j < FM; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+        auto kstep = [&](int kb, auto stage_tag) {
+            constexpr int S = decltype(stage_tag)::value, SN = (S + 1) % NS, SL = (S + NS - 1) % NS;
+            const uint8_t* st = smem + S * STAGE;
+            const uint8_t* nst = smem + SN * STAGE;
+            const unsigned koff1 = koff_of(kb + NS - 1), koff2 = koff_of(kb + NS);
+            __builtin_amdgcn_sched_barrier(0);
+            // activation fragment j, weight fragment i, half h (four of the eight groups).  An accumulator's two matrix
+            // instructions follow each other: FN apart, so that neither would wait for the other, 4096x18432x7168 takes
+            // 263 us instead of 255 (the chip's power is what bounds this kernel, and a chained sum costs less of it).
+#pragma unroll
+            for (int j = 0; j < FM; ++j) {
+                if (j == FM - 1) {
+                    kstep_barrier();
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+#pragma unroll
+                for (int i = 0; i < FN; ++i) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int s = (j * 2 + h) * FN + i;
+                        if (s < C::HEADN) issue_load(cur, C::TAILN + s, SL, koff1);
+                        if (h == 0 && i == 0 && j + 1 < FM) {
+                            qf[(j + 1) & 1] = load_frag(st + q_base + (j + 1) * 2048);
+                            qs[(j + 1) & 1] = read_scale(S, qs_base + (j + 1) * 64);
+                        }
+                        acc[i][j] = mfma_mx4(h ? pf[i].h1 : pf[i].h0, h ? qf[j & 1].h1 : qf[j & 1].h0, acc[i][j], ps[i], qs[j & 1], h);
+                        // (ties it to this point of the K-step)
+                        asm volatile("" : "+v"(acc[i][j]));
+                        if (j == FM - 1 && h == 1) {
+                            pf[i] = load_frag(nst + p_base + i * 2048);
+                            ps[i] = read_scale(SN, ps_base + i * 64);
+#pragma unroll
+                            for (int l = i; l < C::TAILN; l += FN) issue_load(cur, l, S, koff2);
+                            if (i == 0) issue_scales(cur, kb + NS, S);
+                            if (i == FN - 1) {
+                                qf[0] = load_frag(nst + q_base);
+                                qs[0] = read_scale(SN, qs_base);
+                            }
+                        }
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                }
+            }
+        };
+        // The same for a wave whose rows all lie beyond the tile's: it moves its share of the data, in the same order.
+        auto kstep_idle = [&](int kb, auto stage_tag) {
+            constexpr int S = decltype(stage_tag)::value, SL = (S + NS - 1) % NS;
+            const unsigned koff1 = koff_of(kb + NS - 1), koff2 = koff_of(kb + NS);
+#pragma unroll
+            for (int i = 0; i < C::HEADN; ++i) issue_load(cur, C::TAILN + i, SL, koff1);
+            kstep_barrier();
+            issue_load(cur, 0, S, koff2);
+            issue_scales(cur, kb + NS, S);
+#pragma unroll
+            for (int i = 1; i < C::TAILN; ++i) issue_load(cur, i, S, koff2);
+        };
+        using st0 = std::integral_constant<int, 0>;
+        using st1 = std::integral_constant<int, 1>;
+        using st2 = std::integral_constant<int, 2>;
+        const bool active = wm * C::TM < cur.m_rows;    // wave-uniform
+        auto kloop = [&](auto step) {
+            int kb = 0;
+            if constexpr (NS == 2) {
+                for (; kb + 1 < KB; kb += 2) {
+                    step(kb, st0{});
+                    step(kb + 1, st1{});
+                }
+                if (kb < KB) step(kb, st0{});
+            } else {
+                for (; kb + 2 < KB; kb += 3) {
+                    step(kb, st0{});
+                    step(kb + 1, st1{});
+                    step(kb + 2, st2{});
+                }
+                if (kb < KB) step(kb, st0{});
+                if (kb + 1 < KB) step(kb + 1, st1{});
+            }
+        };
+        if (active) kloop(kstep);
+        else kloop(kstep_idle);
+        __builtin_amdgcn_s_waitcnt(0x70);              // nothing is on its way into the stages any more
+        __syncthreads();                               // every wave is done with all of them
+
+        // ---- the next tile's first K-steps fly into stages 0 .. NS-2 during this one's way out ----
+        MxTile nxt;
+        ++unit;
+        const bool more = setup(unit, nxt);
+        if (more) issue_first_steps(nxt);
+        // A lane owns one activation row and, per weight fragment, four consecutive columns: each wave turns 16 rows x
+        // TN columns at a time through an LDS strip of its own in the last stage, so that stores are 16 bytes a lane
+        // and whole 128- or 256-byte row segments (64-byte ones straight from the registers: 257 -> 271 us with
+        // non-temporal stores, 264 with plain ones).
+        // (every address here derives from this copy of the thread index, which the compiler cannot see through: none is
+        // computed before the K-loop and kept in a register across it)
+        int tid_e = threadIdx.x;
+        asm volatile("" : "+v"(tid_e));
+        const int lane = tid_e & 63, l16 = tid_e & 15, g4 = (tid_e >> 4) & 3;
+        constexpr int ESZ = OUT_BF16 ? 2 : 4;
+        constexpr int SEG = C::TN * ESZ, ROWB = SEG + 16, CPR = SEG / 16, PASSES = 16 * CPR / 64;
+        static_assert(16 * CPR % 64 == 0, "epilogue mapping");
+        uint8_t* strip = smem + (NS - 1) * STAGE + wave * (16 * ROWB);
+        uint64_t c_bits = reinterpret_cast<uint64_t>(p.c);
+        int64_t ldc = p.ldc;
+        asm volatile("" : "+s"(c_bits), "+s"(ldc));    // (registers of their own: not re-read in front of every store)
+        uint8_t* c_base = (uint8_t*)(__attribute__((address_space(1))) uint8_t*)c_bits;
+        if (active) {
+#pragma unroll
+            for (int j = 0; j < FM; ++j) {
+                [[maybe_unused]] f32x4 old[PASSES];    // (16 rows further ahead they would not fit beside the sums: 332 -> 355 us)
+                if constexpr (!OUT_BF16) {
+                    if (p.accumulate) {
+#pragma unroll
+                        for (int ps_ = 0; ps_ < PASSES; ++ps_) {
+                            const int idx = ps_ * 64 + lane, ml = wm * C::TM + j * 16 + idx / CPR, nl = wn * C::TN + (idx % CPR) * 4;
+                            old[ps_] = f32x4{0.f, 0.f, 0.f, 0.f};
+                            if (ml < cur.m_rows && nl + 4 <= cur.n_rows)
+                                old[ps_] = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(c_base + ((int64_t)(cur.m0 + ml) * ldc + cur.n0 + nl) * 4));
+                        }
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < FN; ++i) {
+                    const f32x4 v = acc[i][j];
+                    uint8_t* dst = strip + l16 * ROWB + (i * 16 + g4 * 4) * ESZ;
+                    if constexpr (OUT_BF16) *reinterpret_cast<u32x2*>(dst) = u32x2{pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w)};
+                    else *reinterpret_cast<f32x4*>(dst) = v;
+                }
+                __builtin_amdgcn_wave_barrier();       // same-wave LDS accesses complete in order
+                u32x4 wv[PASSES];
+#pragma unroll
+                for (int ps_ = 0; ps_ < PASSES; ++ps_) {
+                    const int idx = ps_ * 64 + lane;
+                    wv[ps_] = *reinterpret_cast<const u32x4*>(strip + (idx / CPR) * ROWB + (idx % CPR) * 16);
+                }
+#pragma unroll
+                for (int ps_ = 0; ps_ < PASSES; ++ps_) {
+                    const int idx = ps_ * 64 + lane;
+                    const int ml = wm * C::TM + j * 16 + idx / CPR, nl = wn * C::TN + (idx % CPR) * (16 / ESZ);
+                    if (ml >= cur.m_rows || nl >= cur.n_rows) continue;
+                    uint8_t* gp = c_base + ((int64_t)(cur.m0 + ml) * ldc + cur.n0 + nl) * ESZ;
+                    const u32x4 w = wv[ps_];
+                    if (nl + 16 / ESZ <= cur.n_rows) {
+                        if constexpr (OUT_BF16) {
+                            __builtin_nontemporal_store(w, reinterpret_cast<u32x4*>(gp));
+                        } else {
+                            f32x4 o = f32x4{as_f32(w.x), as_f32(w.y), as_f32(w.z), as_f32(w.w)};
+                            if (p.accumulate) { const f32x4 v = old[ps_]; o.x += v.x; o.y += v.y; o.z += v.z; o.w += v.w; }
+                            __builtin_nontemporal_store(o, reinterpret_cast<f32x4*>(gp));
+                        }
+                    } else {
+                        const unsigned int wd[4] = {w.x, w.y, w.z, w.w};
+                        for (int q = 0; q < 16 / ESZ && nl + q < cur.n_rows; ++q) {
+                            if constexpr (OUT_BF16) {
+                                reinterpret_cast<uint16_t*>(gp)[q] = (uint16_t)(wd[q >> 1] >> (16 * (q & 1)));
+                            } else {
+                                float* d = reinterpret_cast<float*>(gp) + q;
+                                *d = p.accumulate ? *d + as_f32(wd[q]) : as_f32(wd[q]);
+                            }
+                        }
+                    }
+                }
+                __builtin_amdgcn_wave_barrier();       // the strip is read before the next rows replace it
+            }
+        }
+        if (!more) break;
+        cur = nxt;
+    }
+}
+
 // ---- host side -------------------------------------------------------------------
 template <class C>
 static ds3_status launch_tile(MxGemmParams p, ds3_dtype ct, hipStream_t st) {
@@ -283,10 +694,39 @@ static ds3_status launch_tile(MxGemmParams p, ds3_dtype ct, hipStream_t st) {
     return hipGetLastError() == hipSuccess ? DS3_OK : DS3_ERR_LAUNCH;
 }
 
+// Compute units of the current device, a multiple of 8.
+static int compute_units_x8() {
+    int dev = 0, n = 0;
+    if (hipGetDevice(&dev) != hipSuccess || hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n < 8) return 256;
+    return n / 8 * 8;
+}
+
+template <class C>
+static ds3_status launch_main(MxGemmParams p, ds3_dtype ct, int cus, hipStream_t st) {
+    p.tiles_m = (p.M + C::BM - 1) / C::BM;
+    if (p.G > 0) p.tiles_m = (int)std::min<int64_t>((int64_t)p.tiles_m + p.G, p.M);     // (an upper bound)
+    p.tiles_n = (p.N + C::BN - 1) / C::BN;
+    const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n, want = (tiles + 7) / 8 * 8, slots = (int64_t)cus * C::WG_PER_CU;
+    if (tiles > (1ll << 31) - 16) return DS3_ERR_UNSUPPORTED;
+    const dim3 grid((unsigned)std::min(want, slots)), block(C::NT);
+    (void)hipGetLastError();                            // a stale error of earlier, unrelated work is not this launch's
+    if (p.G > 0) {
+        if (ct == DS3_BF16) gemm_mxfp4_kernel<C, true, true><<<grid, block, 0, st>>>(p);
+        else gemm_mxfp4_kernel<C, false, true><<<grid, block, 0, st>>>(p);
+    } else {
+        if (ct == DS3_BF16) gemm_mxfp4_kernel<C, true, false><<<grid, block, 0, st>>>(p);
+        else gemm_mxfp4_kernel<C, false, false><<<grid, block, 0, st>>>(p);
+    }
+    return hipGetLastError() == hipSuccess ? DS3_OK : DS3_ERR_LAUNCH;
+}
+
 ds3_status launch_gemm_mxfp4(const MxGemmParams& p, ds3_dtype ct, hipStream_t st) {
     // 32-bit offsets inside a tile of up to 256 rows
     if ((int64_t)257 * p.ldb + p.K / 2 >= (1ll << 31) || (int64_t)257 * p.lda + p.K / 2 >= (1ll << 31)) return DS3_ERR_UNSUPPORTED;
+    const int cus = compute_units_x8();
     const int64_t rows = p.G > 0 ? (p.M + p.G - 1) / p.G : p.M;
+    if (p.G == 0 && (int64_t)((p.M + 255) / 256) * ((p.N + 255) / 256) * 8 >= 5 * (int64_t)cus) return launch_main<MainCfg<256, 256, 4, 2, 2>>(p, ct, cus, st);
+    if (p.G > 0 && rows > 64) return launch_main<MainCfg<256, 128, 4, 2, 3>>(p, ct, cus, st);
     if (rows <= 32) return launch_tile<TileCfg<2, 2, 4, 1, 3>>(p, ct, st);
     return launch_tile<TileCfg<2, 8, 4, 1, 3>>(p, ct, st);
 }
