@@ -26,9 +26,10 @@ struct SortParams {
     int32_t* rows;
 };
 
-// expert of choice p among those held here, or -1
+// Expert of choice i among those held here, or -1.  PACKED: rows of ids without gaps on a 16-byte border.
+template <bool PACKED>
 __device__ __forceinline__ int sort_expert(const SortParams& p, int i) {
-    const int64_t at = p.ld == p.top_k ? (int64_t)i : (int64_t)(i / p.top_k) * p.ld + i % p.top_k;
+    const int64_t at = PACKED || p.ld == p.top_k ? (int64_t)i : (int64_t)(i / p.top_k) * p.ld + i % p.top_k;
     const unsigned int e = (unsigned int)p.ids[at] - (unsigned int)p.first;
     return e < (unsigned int)p.G ? (int)e : -1;
 }
@@ -51,12 +52,13 @@ __device__ __forceinline__ int block_exclusive(int v, int* part) {
 
 // Places choices [i0, i1) (at most kSortChunk) in order: base[g] is the next free row of expert g.  Within a wave the
 // lanes of the same expert find each other by a ballot per bit of its number; the waves take turns.
+template <bool PACKED>
 __device__ __forceinline__ void place(const SortParams& p, int i0, int i1, int* base) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int bits = 32 - __clz(p.G);
     for (int at = i0; at < i1; at += kSortThreads) {
         const int i = at + (int)threadIdx.x;
-        const int e = i < i1 ? sort_expert(p, i) : -1;
+        const int e = i < i1 ? sort_expert<PACKED>(p, i) : -1;
         unsigned long long same = __ballot(e >= 0);
         for (int b = 0; b < bits; ++b) {
             const unsigned long long set = __ballot((e >> b) & 1);
@@ -77,47 +79,93 @@ __device__ __forceinline__ void place(const SortParams& p, int i0, int i1, int* 
 }
 
 // One launch: every workgroup counts all choices, those before its own 1024 apart, so none waits for another.
+template <bool PACKED>
 __global__ __launch_bounds__(kSortThreads) void moe_sort_kernel(const SortParams p) {
     __shared__ int before[kSortMaxGroups + 1], total[kSortMaxGroups + 1], part[kSortThreads / 64];
     const int tid = threadIdx.x, start = (int)blockIdx.x * kSortThreads;
     before[tid] = 0;
     total[tid] = 0;
+    // few experts: several copies of each count, a lane's own, or the lanes of a wave wait for each other (65536 choices
+    // of 8 experts 17 us)
+    const int shift = min(4, __clz(p.G | 1) - 22), copy = tid & ((1 << shift) - 1);       // 2^shift copies of at most 1023 counts
     __syncthreads();
-    for (int i = tid; i < p.n; i += kSortThreads) {
-        const int e = sort_expert(p, i);
-        if (e >= 0) atomicAdd(i < start ? &before[e] : &total[e], 1);
+    if constexpr (PACKED) {
+        // four choices a load, eight loads in flight
+        constexpr int AHEAD = 8, BATCH = 4 * AHEAD * kSortThreads;
+        for (int b = 0; b < p.n; b += BATCH) {
+            i32x4 v[AHEAD];
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                const int i = b + (k * kSortThreads + tid) * 4;
+                v[k] = i32x4{-1, -1, -1, -1} + p.first;                   // (no expert held here)
+                if (i + 4 <= p.n) v[k] = *reinterpret_cast<const i32x4*>(p.ids + i);
+                else for (int q = 0; i + q < p.n; ++q) v[k][q] = p.ids[i + q];
+            }
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                int* const cnt = (b + (k * kSortThreads + tid) * 4 < start ? before : total) + copy;    // (`start` is a multiple of four)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const unsigned int e = (unsigned int)v[k][q] - (unsigned int)p.first;
+                    if (e < (unsigned int)p.G) atomicAdd(&cnt[e << shift], 1);
+                }
+            }
+        }
+    } else {
+        constexpr int AHEAD = 8;
+        for (int b = 0; b < p.n; b += AHEAD * kSortThreads) {
+            int e[AHEAD];
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                const int i = b + k * kSortThreads + tid;
+                e[k] = i < p.n ? sort_expert<PACKED>(p, i) : -1;
+            }
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k)
+                if (e[k] >= 0) atomicAdd((b + k * kSortThreads < start ? before : total) + ((e[k] << shift) + copy), 1);
+        }
     }
     __syncthreads();
-    const int all = tid < p.G ? before[tid] + total[tid] : 0;
-    const int off = block_exclusive(all, part);
-    if (tid < p.G) before[tid] += off;
+    int all = 0, mine = 0;
+    if (tid < p.G) {
+        for (int c = 0; c < 1 << shift; ++c) {
+            mine += before[(tid << shift) + c];
+            all += total[(tid << shift) + c];
+        }
+        all += mine;
+    }
+    const int off = block_exclusive(all, part);        // (its barrier: the copies are summed before the sums replace them)
+    if (tid < p.G) before[tid] = mine + off;
     if (blockIdx.x == 0 && tid <= p.G) p.offsets[tid] = off;     // (thread G holds no expert: the sum of all)
     __syncthreads();
-    place(p, start, min(start + kSortThreads, p.n), before);
+    place<PACKED>(p, start, min(start + kSortThreads, p.n), before);
 }
 
 // The long form, for more choices than each workgroup should count: chunks are counted, the counts summed up over the
 // chunks, and the chunks placed.  A chunk's counts, then its first free rows, lie where its rows will be (a chunk has at
 // least as many choices as there are experts); the last chunk, which may be shorter, is counted where it is needed.
+template <bool PACKED>
 __device__ __forceinline__ void count_chunk(const SortParams& p, int chunk, int* cnt) {
     cnt[threadIdx.x] = 0;
     __syncthreads();
     const int end = min((chunk + 1) * kSortChunk, p.n);
     for (int i = chunk * kSortChunk + (int)threadIdx.x; i < end; i += kSortThreads) {
-        const int e = sort_expert(p, i);
+        const int e = sort_expert<PACKED>(p, i);
         if (e >= 0) atomicAdd(&cnt[e], 1);
     }
     __syncthreads();
 }
+template <bool PACKED>
 __global__ __launch_bounds__(kSortThreads) void moe_sort_count_kernel(const SortParams p) {
     __shared__ int cnt[kSortMaxGroups + 1];
-    count_chunk(p, blockIdx.x, cnt);
+    count_chunk<PACKED>(p, blockIdx.x, cnt);
     if ((int)threadIdx.x < p.G) p.rows[(int64_t)blockIdx.x * kSortChunk + threadIdx.x] = cnt[threadIdx.x];
 }
+template <bool PACKED>
 __global__ __launch_bounds__(kSortThreads) void moe_sort_scan_kernel(const SortParams p, int chunks) {
     __shared__ int cnt[kSortMaxGroups + 1], part[kSortThreads / 64];
     const int tid = threadIdx.x;
-    count_chunk(p, chunks - 1, cnt);
+    count_chunk<PACKED>(p, chunks - 1, cnt);
     int sum = 0;
     if (tid < p.G) {
         constexpr int AHEAD = 16;                      // counts in flight: one after another each would wait out a latency
@@ -136,17 +184,18 @@ __global__ __launch_bounds__(kSortThreads) void moe_sort_scan_kernel(const SortP
     const int off = block_exclusive(sum, part);
     if (tid <= p.G) p.offsets[tid] = off;
 }
+template <bool PACKED>
 __global__ __launch_bounds__(kSortThreads) void moe_sort_place_kernel(const SortParams p, int chunks) {
     __shared__ int base[kSortMaxGroups + 1];
     const int tid = threadIdx.x, chunk = blockIdx.x;
     if (chunk == chunks - 1) {
-        count_chunk(p, chunk, base);
+        count_chunk<PACKED>(p, chunk, base);
         if (tid < p.G) base[tid] = p.offsets[tid + 1] - base[tid];
     } else if (tid < p.G) {
         base[tid] = p.offsets[tid] + p.rows[(int64_t)chunk * kSortChunk + tid];
     }
     __syncthreads();                                   // (the counts are read before the first rows are written over them)
-    place(p, chunk * kSortChunk, min((chunk + 1) * kSortChunk, p.n), base);
+    place<PACKED>(p, chunk * kSortChunk, min((chunk + 1) * kSortChunk, p.n), base);
 }
 
 // =============================================================================
@@ -170,229 +219,274 @@ template <> __device__ __forceinline__ void store8<F32>(uint8_t* p, const float*
 template <typename T> __device__ __forceinline__ int64_t bytes_of(int64_t n) { return n * (16 / T::EPL); }
 
 // =============================================================================
-// Dispatch: a workgroup takes 2048 columns of one token, a lane eight of them (one 1x128 tile or 128-element block is 16
-// lanes); what it leaves is written to every row of the token's choices.
+// Dispatch: a wave takes NG * 512 columns of one token, a lane eight of each 512 (one 1x128 tile or 128-element block is
+// 16 lanes); what it leaves is written to every row of the token's choices.
 // =============================================================================
-template <typename T, DispatchTo TO>
+template <typename T, DispatchTo TO, int NG>
 __global__ __launch_bounds__(256) void moe_dispatch_kernel(const DispatchParams p, int segs) {
     const int lane = threadIdx.x & 63, lane16 = threadIdx.x & 15;
-    const int64_t token = blockIdx.x / (unsigned)segs;
-    const int64_t col = (int64_t)(blockIdx.x % (unsigned)segs) * 2048 + threadIdx.x * 8;
+    const unsigned int task = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+    const int64_t token = task / (unsigned)segs;
+    if (token >= p.tokens) return;
+    const int64_t col0 = (int64_t)(task % (unsigned)segs) * (NG * 512) + lane * 8;
     int row;
-    unsigned long long todo = token_rows(p.row_of_slot, token, p.top_k, p.total_rows, lane, row);
-    if (todo == 0) return;
-    Granule8<T> g;
-    g.load(p.x + token * p.ldx_bytes + bytes_of<T>(col), p.cols - col);
-    const int64_t left = p.cols - col;
-    if constexpr (TO == kDispatchRows) {
-        for (; todo; todo &= todo - 1) {
-            const int64_t r = __builtin_amdgcn_readlane(row, __builtin_ctzll(todo));
-            uint8_t* dst = p.y + r * p.ldy_bytes + bytes_of<T>(col);
+    const unsigned long long here = token_rows(p.row_of_slot, token, p.top_k, p.total_rows, lane, row);
+    if (here == 0) return;
+    Granule8<T> g[NG];
 #pragma unroll
-            for (int h = 0; h < Granule8<T>::N; ++h)
-                if (h * T::EPL < left) st_stream(dst + h * 16, g.g[h]);
+    for (int c = 0; c < NG; ++c) g[c].load(p.x + token * p.ldx_bytes + bytes_of<T>(col0 + c * 512), p.cols - col0 - c * 512);
+    if constexpr (TO == kDispatchRows) {
+        for (unsigned long long todo = here; todo; todo &= todo - 1) {
+            const int64_t r = __builtin_amdgcn_readlane(row, __builtin_ctzll(todo));
+#pragma unroll
+            for (int c = 0; c < NG; ++c) {
+                const int64_t col = col0 + c * 512;
+                uint8_t* dst = p.y + r * p.ldy_bytes + bytes_of<T>(col);
+#pragma unroll
+                for (int h = 0; h < Granule8<T>::N; ++h)
+                    if (col + h * T::EPL < p.cols) st_stream(dst + h * 16, g[c].g[h]);
+            }
         }
     } else {
-        float v[8];
-        g.values(v);
-        unsigned int w0, w1 = 0, sw;
-        if constexpr (TO == kDispatchFp8) {
-            const GroupScale gs = group_scale(as_f32(row16_max_bits(g.amax_bits())), p.pow2);
+        unsigned int w0[NG], w1[NG], sw[NG];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = v[i] * gs.r;
-            w0 = cvt4_e4m3(v[0], v[1], v[2], v[3]);
-            w1 = cvt4_e4m3(v[4], v[5], v[6], v[7]);
-            sw = as_u32(gs.s);
-        } else {
-            const MxScale ms = mx_scale(quad_max_bits(g.amax_bits()));
-            w0 = cvt8_e2m1(v, ms.r);
-            sw = row16_scale_word(ms.e, lane16);
-        }
-        const int64_t kb = col >> 7;
-        for (; todo; todo &= todo - 1) {
-            const int64_t r = __builtin_amdgcn_readlane(row, __builtin_ctzll(todo));
+        for (int c = 0; c < NG; ++c) {
+            float v[8];
+            g[c].values(v);
             if constexpr (TO == kDispatchFp8) {
-                uint8_t* dst = p.y + r * p.ldy_bytes + col;
-                if (left >= 8) st_stream(dst, u32x2{w0, w1});
-                else if (left > 0) st_stream(dst, w0);
+                const GroupScale gs = group_scale(as_f32(row16_max_bits(g[c].amax_bits())), p.pow2);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = v[i] * gs.r;
+                w0[c] = cvt4_e4m3(v[0], v[1], v[2], v[3]);
+                w1[c] = cvt4_e4m3(v[4], v[5], v[6], v[7]);
+                sw[c] = as_u32(gs.s);
             } else {
-                uint8_t* dst = p.y + r * p.ldy_bytes + (col >> 1);
-                if (left >= 8) st_stream(dst, w0);
-                else if (left > 0) st_stream(dst, (uint16_t)w0);
+                const MxScale ms = mx_scale(quad_max_bits(g[c].amax_bits()));
+                w0[c] = cvt8_e2m1(v, ms.r);
+                sw[c] = row16_scale_word(ms.e, lane16);
             }
-            if (lane16 == 0 && left > 0) static_cast<uint32_t*>(p.s)[r * p.ssr + kb * p.ssk] = sw;
+        }
+        for (unsigned long long todo = here; todo; todo &= todo - 1) {
+            const int64_t r = __builtin_amdgcn_readlane(row, __builtin_ctzll(todo));
+#pragma unroll
+            for (int c = 0; c < NG; ++c) {
+                const int64_t col = col0 + c * 512, left = p.cols - col;
+                if (left <= 0) break;
+                if constexpr (TO == kDispatchFp8) {
+                    uint8_t* dst = p.y + r * p.ldy_bytes + col;
+                    if (left >= 8) st_stream(dst, u32x2{w0[c], w1[c]});
+                    else st_stream(dst, w0[c]);
+                } else {
+                    uint8_t* dst = p.y + r * p.ldy_bytes + (col >> 1);
+                    if (left >= 8) st_stream(dst, w0[c]);
+                    else st_stream(dst, (uint16_t)w0[c]);
+                }
+                if (lane16 == 0) static_cast<uint32_t*>(p.s)[r * p.ssr + (col >> 7) * p.ssk] = sw[c];
+            }
         }
     }
 }
 
 // =============================================================================
-// Combine: the same split; up to four of the rows are in flight at a time.
+// Combine: the same split; NR rows are in flight at a time.
 // =============================================================================
-template <typename TY, typename TO>
+template <typename TY, typename TO, int NG>
 __global__ __launch_bounds__(256) void moe_combine_kernel(const CombineParams p, int segs) {
+    constexpr int NR = 4;
     const int lane = threadIdx.x & 63;
-    const int64_t token = blockIdx.x / (unsigned)segs;
-    const int64_t col = (int64_t)(blockIdx.x % (unsigned)segs) * 2048 + threadIdx.x * 8;
+    const unsigned int task = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+    const int64_t token = task / (unsigned)segs;
+    if (token >= p.tokens) return;
+    const int64_t col0 = (int64_t)(task % (unsigned)segs) * (NG * 512) + lane * 8;
     int row;
     unsigned long long todo = token_rows(p.row_of_slot, token, p.top_k, p.total_rows, lane, row);
     float weight = 1.f;
     if (p.w != nullptr && lane < p.top_k) weight = p.w[token * p.top_k + lane];
-    const int64_t left = p.cols - col;
-    const uint8_t* y = p.y + bytes_of<TY>(col);
-    float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    float acc[NG][8];
+#pragma unroll
+    for (int c = 0; c < NG; ++c)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[c][e] = 0.f;
     while (todo) {
-        Granule8<TY> g[4];
-        float w[4];
+        Granule8<TY> g[NR][NG];
+        float w[NR];
         int n = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < NR; ++i) {
             if (todo) {
                 const int s = __builtin_ctzll(todo);
                 todo &= todo - 1;
                 w[i] = as_f32((unsigned int)__builtin_amdgcn_readlane((int)as_u32(weight), s));
-                g[i].load(y + (int64_t)__builtin_amdgcn_readlane(row, s) * p.ldy_bytes, left);
+                const uint8_t* y = p.y + (int64_t)__builtin_amdgcn_readlane(row, s) * p.ldy_bytes;
+#pragma unroll
+                for (int c = 0; c < NG; ++c) g[i][c].load(y + bytes_of<TY>(col0 + c * 512), p.cols - col0 - c * 512);
                 n = i + 1;
             }
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < NR; ++i) {
             if (i < n) {
-                float v[8];
-                g[i].values(v);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) acc[e] = __builtin_fmaf(w[i], v[e], acc[e]);
+                for (int c = 0; c < NG; ++c) {
+                    float v[8];
+                    g[i][c].values(v);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) acc[c][e] = __builtin_fmaf(w[i], v[e], acc[c][e]);
+                }
             }
         }
     }
-    store8<TO>(p.out + token * p.ldo_bytes + bytes_of<TO>(col), acc, left);
+#pragma unroll
+    for (int c = 0; c < NG; ++c)
+        store8<TO>(p.out + token * p.ldo_bytes + bytes_of<TO>(col0 + c * 512), acc[c], p.cols - col0 - c * 512);
 }
 
 // =============================================================================
-// Combine's gradients: a workgroup takes a token.  dy of each row is the weight times the token's gradient, dw the
-// product of the two rows: lane by lane over the columns, then over the lanes and waves, always in the same order.
+// Combine's gradients: a wave takes a choice, the choices of a token side by side, so that the token's gradient comes
+// from memory once.  dy is the weight times that gradient; dw is summed lane by lane over the columns, then over the
+// lanes, always in the same order.
 // =============================================================================
 template <typename TY, typename TO>
 __global__ __launch_bounds__(256) void moe_combine_bwd_kernel(const CombineParams p) {
-    constexpr int NC = 4;                              // 8-column pieces a thread keeps of the gradient
-    __shared__ float dots[64][4];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t token = blockIdx.x;
-    int row;
-    const unsigned long long here = token_rows(p.row_of_slot, token, p.top_k, p.total_rows, lane, row);
-    float weight = 1.f;
-    if (p.w != nullptr && lane < p.top_k) weight = p.w[token * p.top_k + lane];
-    if (here != 0) {
-        for (int64_t c0 = 0; c0 < p.cols; c0 += 2048 * NC) {
-            Granule8<TO> d[NC];
+    constexpr int NG = 4;
+    const int lane = threadIdx.x & 63;
+    const int64_t choice = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (choice >= p.tokens * p.top_k) return;
+    const int64_t token = (unsigned int)choice / (unsigned int)p.top_k;
+    const int64_t r = p.row_of_slot[choice];
+    float dot = 0.f;
+    if (r >= 0 && r < p.total_rows) {
+        const float w = p.w != nullptr ? p.w[choice] : 1.f;
+        const uint8_t* const d = p.out + token * p.ldo_bytes;
+        const uint8_t* const y = p.y + r * p.ldy_bytes;
+        uint8_t* const dy = p.dy + r * p.lddy_bytes;
+        for (int64_t c0 = lane * 8; c0 < p.cols; c0 += NG * 512) {
+            Granule8<TO> dg[NG];
+            Granule8<TY> yg[NG];
 #pragma unroll
-            for (int c = 0; c < NC; ++c) {
-                const int64_t col = c0 + c * 2048 + threadIdx.x * 8;
-                d[c].load(p.out + token * p.ldo_bytes + bytes_of<TO>(col), p.cols - col);
-            }
-            for (unsigned long long todo = here; todo; todo &= todo - 1) {
-                const int s = __builtin_ctzll(todo);
-                const int64_t r = __builtin_amdgcn_readlane(row, s);
-                const float w = as_f32((unsigned int)__builtin_amdgcn_readlane((int)as_u32(weight), s));
-                Granule8<TY> g[NC];
+            for (int c = 0; c < NG; ++c) dg[c].load_kept(d + bytes_of<TO>(c0 + c * 512), p.cols - c0 - c * 512);
 #pragma unroll
-                for (int c = 0; c < NC; ++c) {
-                    const int64_t col = c0 + c * 2048 + threadIdx.x * 8;
-                    g[c].load(p.y + r * p.ldy_bytes + bytes_of<TY>(col), p.cols - col);
+            for (int c = 0; c < NG; ++c) yg[c].load(y + bytes_of<TY>(c0 + c * 512), p.cols - c0 - c * 512);
+#pragma unroll
+            for (int c = 0; c < NG; ++c) {
+                float dv[8], yv[8];
+                dg[c].values(dv);
+                yg[c].values(yv);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    dot = __builtin_fmaf(dv[e], yv[e], dot);
+                    dv[e] *= w;
                 }
-                float dot = 0.f;
-#pragma unroll
-                for (int c = 0; c < NC; ++c) {
-                    const int64_t col = c0 + c * 2048 + threadIdx.x * 8;
-                    float dv[8], yv[8];
-                    d[c].values(dv);
-                    g[c].values(yv);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        dot = __builtin_fmaf(dv[e], yv[e], dot);
-                        dv[e] *= w;
-                    }
-                    store8<TY>(p.dy + r * p.lddy_bytes + bytes_of<TY>(col), dv, p.cols - col);
-                }
-#pragma unroll
-                for (int m = 1; m < 64; m <<= 1) dot += __shfl_xor(dot, m);
-                if (lane == 0) dots[s][wave] = c0 == 0 ? dot : dots[s][wave] + dot;
+                store8<TY>(dy + bytes_of<TY>(c0 + c * 512), dv, p.cols - c0 - c * 512);
             }
         }
+#pragma unroll
+        for (int m = 1; m < 64; m <<= 1) dot += __shfl_xor(dot, m);
     }
-    __syncthreads();
-    if ((int)threadIdx.x < p.top_k) {
-        const int s = threadIdx.x;
-        float v = 0.f;
-        if ((here >> s) & 1) v = ((dots[s][0] + dots[s][1]) + dots[s][2]) + dots[s][3];
-        p.dw[token * p.top_k + s] = v;
-    }
+    if (lane == 0) p.dw[choice] = dot;
 }
 
 // ---- host side -------------------------------------------------------------------
 static ds3_status launch_status() { return hipGetLastError() == hipSuccess ? DS3_OK : DS3_ERR_LAUNCH; }
 constexpr int64_t kMaxGrid = (1ll << 24) - 1;          // a grid may have 2^32 threads
 
-// Up to here every workgroup counts all choices itself.
-constexpr int kSortOneLaunch = 65536;
+// Up to here every workgroup counts all choices itself (65536 of 256 experts 10 us, of which 32 are here 8; the long form
+// takes three launches, of 4, 4 and 13 us at 65536).  Below the second line four choices a load do not pay for the longer
+// kernel (32 choices: 3.4 / 4.6 us, 16384: 8.0 / 7.2, 65536: 17 / 10).
+constexpr int kSortOneLaunch = 131072, kSortPacked = 8192;
+
+template <bool PACKED>
+static ds3_status sort_as(const SortParams& p, hipStream_t st) {
+    (void)hipGetLastError();                            // a stale error of earlier, unrelated work is not this launch's
+    if (p.n <= kSortOneLaunch) {
+        const int blocks = std::max(1, (p.n + kSortThreads - 1) / kSortThreads);
+        moe_sort_kernel<PACKED><<<dim3(blocks), kSortThreads, 0, st>>>(p);
+        return launch_status();
+    }
+    const int chunks = (p.n + kSortChunk - 1) / kSortChunk;
+    moe_sort_count_kernel<PACKED><<<dim3(chunks - 1), kSortThreads, 0, st>>>(p);
+    moe_sort_scan_kernel<PACKED><<<dim3(1), kSortThreads, 0, st>>>(p, chunks);
+    moe_sort_place_kernel<PACKED><<<dim3(chunks), kSortThreads, 0, st>>>(p, chunks);
+    return launch_status();
+}
 
 ds3_status launch_moe_sort(const int32_t* ids, int64_t tokens, int top_k, int64_t ld, int first, int G, int32_t* offsets,
                            int32_t* row_of_slot, hipStream_t st) {
     const SortParams p{ids, ld, (int)(tokens * top_k), top_k, first, G, offsets, row_of_slot};
-    (void)hipGetLastError();                            // a stale error of earlier, unrelated work is not this launch's
-    if (p.n <= kSortOneLaunch) {
-        const int blocks = std::max(1, (p.n + kSortThreads - 1) / kSortThreads);
-        moe_sort_kernel<<<dim3(blocks), kSortThreads, 0, st>>>(p);
-        return launch_status();
-    }
-    const int chunks = (p.n + kSortChunk - 1) / kSortChunk;
-    moe_sort_count_kernel<<<dim3(chunks - 1), kSortThreads, 0, st>>>(p);
-    moe_sort_scan_kernel<<<dim3(1), kSortThreads, 0, st>>>(p, chunks);
-    moe_sort_place_kernel<<<dim3(chunks), kSortThreads, 0, st>>>(p, chunks);
-    return launch_status();
+    const bool packed = ld == top_k && (reinterpret_cast<uintptr_t>(ids) & 15u) == 0 && p.n > kSortPacked;
+    return packed ? sort_as<true>(p, st) : sort_as<false>(p, st);
+}
+
+template <typename T, int NG>
+static void dispatch_as(const DispatchParams& p, DispatchTo to, unsigned grid, int segs, hipStream_t st) {
+    if (to == kDispatchRows) moe_dispatch_kernel<T, kDispatchRows, NG><<<dim3(grid), 256, 0, st>>>(p, segs);
+    else if (to == kDispatchFp8) moe_dispatch_kernel<T, kDispatchFp8, NG><<<dim3(grid), 256, 0, st>>>(p, segs);
+    else moe_dispatch_kernel<T, kDispatchMx4, NG><<<dim3(grid), 256, 0, st>>>(p, segs);
+}
+
+// Columns a wave takes, in units of 512: the more, the more is in flight and the fewer waves look up a token's rows; few
+// tokens want more waves.  us with 1 / 2 / 4 units, 7168 columns: FP8, 8192 tokens with one row each on average 35 / 29 / 30,
+// MXFP4 33 / 26 / 24, eight rows each 93 / 95 / 96; 64 tokens 4.0 / 4.3 / 5.3; 2048 columns of FP8 17.4 / 17.1 / 14.7.
+static int columns_per_wave(int64_t tokens, int64_t cols) {
+    const int64_t units = (cols + 511) / 512;
+    return tokens * units < 4096 ? 1 : units >= 3 ? 4 : units >= 2 ? 2 : 1;
+}
+// Workgroups of four waves for every token's columns; 0: more than a grid holds.
+static unsigned wave_grid(int64_t tokens, int64_t cols, int ng, int* segs) {
+    const int64_t s = (cols + ng * 512 - 1) / (ng * 512);
+    if (s > kMaxGrid || tokens > kMaxGrid * 4 / s) return 0;
+    *segs = (int)s;
+    return (unsigned)((tokens * s + 3) / 4);
 }
 
 ds3_status launch_moe_dispatch(const DispatchParams& p, ds3_dtype xt, DispatchTo to, hipStream_t st) {
-    const int64_t segs = (p.cols + 2047) / 2048, n = p.tokens * segs;
-    if (n > kMaxGrid) return DS3_ERR_UNSUPPORTED;
+    int ng = columns_per_wave(p.tokens, p.cols);
+    // (rows as they are, about one a token: 8192 x 7168 BF16 37 / 38 / 40 us with 1 / 2 / 4 units; eight a token 211 / 212 / 208)
+    if (to == kDispatchRows && p.total_rows < 2 * p.tokens) ng = std::min(ng, 2);
+    int segs;
+    const unsigned grid = wave_grid(p.tokens, p.cols, ng, &segs);
+    if (grid == 0) return DS3_ERR_UNSUPPORTED;
     (void)hipGetLastError();
-    const dim3 grid((unsigned)n);
-    const bool b = xt == DS3_BF16;
-    switch (to) {
-        case kDispatchRows:
-            if (b) moe_dispatch_kernel<Bf16, kDispatchRows><<<grid, 256, 0, st>>>(p, (int)segs);
-            else moe_dispatch_kernel<F32, kDispatchRows><<<grid, 256, 0, st>>>(p, (int)segs);
-            break;
-        case kDispatchFp8:
-            if (b) moe_dispatch_kernel<Bf16, kDispatchFp8><<<grid, 256, 0, st>>>(p, (int)segs);
-            else moe_dispatch_kernel<F32, kDispatchFp8><<<grid, 256, 0, st>>>(p, (int)segs);
-            break;
-        case kDispatchMx4:
-            if (b) moe_dispatch_kernel<Bf16, kDispatchMx4><<<grid, 256, 0, st>>>(p, (int)segs);
-            else moe_dispatch_kernel<F32, kDispatchMx4><<<grid, 256, 0, st>>>(p, (int)segs);
-            break;
+    if (xt == DS3_BF16) {
+        if (ng == 4) dispatch_as<Bf16, 4>(p, to, grid, segs, st);
+        else if (ng == 2) dispatch_as<Bf16, 2>(p, to, grid, segs, st);
+        else dispatch_as<Bf16, 1>(p, to, grid, segs, st);
+    } else {
+        if (ng == 4) dispatch_as<F32, 4>(p, to, grid, segs, st);
+        else if (ng == 2) dispatch_as<F32, 2>(p, to, grid, segs, st);
+        else dispatch_as<F32, 1>(p, to, grid, segs, st);
     }
     return launch_status();
 }
 
+template <typename TY, typename TO>
+static void combine_as(const CombineParams& p, int ng, unsigned grid, int segs, hipStream_t st) {
+    if (ng == 1) moe_combine_kernel<TY, TO, 1><<<dim3(grid), 256, 0, st>>>(p, segs);
+    else moe_combine_kernel<TY, TO, 2><<<dim3(grid), 256, 0, st>>>(p, segs);
+}
+
 ds3_status launch_moe_combine(const CombineParams& p, ds3_dtype yt, ds3_dtype ot, hipStream_t st) {
-    const int64_t segs = (p.cols + 2047) / 2048, n = p.tokens * segs;
-    if (n > kMaxGrid) return DS3_ERR_UNSUPPORTED;
+    // (8192 tokens of 7168 columns with one row each on average, 1 / 2 units: 47 / 43 us; 64 tokens with eight 4.3 / 5.3)
+    const int ng = std::min(2, columns_per_wave(p.tokens, p.cols));
+    int segs;
+    const unsigned grid = wave_grid(p.tokens, p.cols, ng, &segs);
+    if (grid == 0) return DS3_ERR_UNSUPPORTED;
     (void)hipGetLastError();
-    const dim3 grid((unsigned)n);
     if (yt == DS3_BF16) {
-        if (ot == DS3_BF16) moe_combine_kernel<Bf16, Bf16><<<grid, 256, 0, st>>>(p, (int)segs);
-        else moe_combine_kernel<Bf16, F32><<<grid, 256, 0, st>>>(p, (int)segs);
+        if (ot == DS3_BF16) combine_as<Bf16, Bf16>(p, ng, grid, segs, st);
+        else combine_as<Bf16, F32>(p, ng, grid, segs, st);
     } else {
-        if (ot == DS3_BF16) moe_combine_kernel<F32, Bf16><<<grid, 256, 0, st>>>(p, (int)segs);
-        else moe_combine_kernel<F32, F32><<<grid, 256, 0, st>>>(p, (int)segs);
+        if (ot == DS3_BF16) combine_as<F32, Bf16>(p, ng, grid, segs, st);
+        else combine_as<F32, F32>(p, ng, grid, segs, st);
     }
     return launch_status();
 }
 
 ds3_status launch_moe_combine_bwd(const CombineParams& p, ds3_dtype yt, ds3_dtype ot, hipStream_t st) {
-    if (p.tokens > kMaxGrid) return DS3_ERR_UNSUPPORTED;
+    const int64_t n = (p.tokens * p.top_k + 3) / 4;
+    if (n > kMaxGrid) return DS3_ERR_UNSUPPORTED;
     (void)hipGetLastError();
-    const dim3 grid((unsigned)p.tokens);
+    const dim3 grid((unsigned)n);
     if (yt == DS3_BF16) {
         if (ot == DS3_BF16) moe_combine_bwd_kernel<Bf16, Bf16><<<grid, 256, 0, st>>>(p);
         else moe_combine_bwd_kernel<Bf16, F32><<<grid, 256, 0, st>>>(p);

@@ -60,6 +60,14 @@ template <typename T> struct Granule8 {
             if (h * T::EPL < left) g[h] = ld_stream(p + h * 16);
         }
     }
+    // ... of what other waves read too
+    __device__ __forceinline__ void load_kept(const uint8_t* p, int64_t left) {
+#pragma unroll
+        for (int h = 0; h < N; ++h) {
+            g[h] = u32x4{0u, 0u, 0u, 0u};
+            if (h * T::EPL < left) g[h] = *reinterpret_cast<const u32x4*>(p + h * 16);
+        }
+    }
     __device__ __forceinline__ unsigned int amax_bits() const {
         unsigned int m = granule_amax_bits<T>(g[0]);
         if constexpr (N == 2) m = umax(m, granule_amax_bits<T>(g[1]));

@@ -105,7 +105,7 @@ def test_expert_order(pkg, mem):
             assert _try(fn, good, **bad) == ALIGN, bad
         assert _try(fn, good, k=65) == UNSUPPORTED and _try(fn, good, total=1 << 31) == UNSUPPORTED
         assert _try(fn, good, tokens=0, x=None) == 0 and _try(fn, good, total=0, x=None) == 0 and _try(fn, good, cols=0) == 0
-        assert _try(fn, good, tokens=1 << 25, cols=8) == UNSUPPORTED           # more workgroups than a grid holds
+        assert _try(fn, good, tokens=1 << 27, cols=8) == UNSUPPORTED           # more workgroups than a grid holds
     good = dict(y=mem, yt=1, total=16, cols=128, ldy=128, rows=mem, w=mem, tokens=8, k=2, out=mem, ot=1, ldo=128, st=None)
     fn = L.ds3_moe_combine
     for key in ("y", "rows", "out"):
@@ -122,7 +122,7 @@ def test_expert_order(pkg, mem):
     for key in ("d", "y", "rows", "dy", "dw"):
         assert _try(fn, good, **{key: None}) == NULL
     assert _try(fn, good, yt=2) == DTYPE and _try(fn, good, lddy=120) == SHAPE and _try(fn, good, lddy=132) == ALIGN
-    assert _try(fn, good, dy=mem + 8) == ALIGN and _try(fn, good, dw=mem + 2) == ALIGN and _try(fn, good, tokens=1 << 24) == UNSUPPORTED
+    assert _try(fn, good, dy=mem + 8) == ALIGN and _try(fn, good, dw=mem + 2) == ALIGN and _try(fn, good, tokens=1 << 27) == UNSUPPORTED
 
 
 def test_python_calls_ask_for_tensors_of_the_current_device(pkg):
