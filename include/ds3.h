@@ -576,6 +576,14 @@ ds3_status ds3_grouped_gemm_mxfp4(int32_t G, const int32_t* group_offsets, int64
                                   void* c, ds3_dtype ct, int64_t ldc, void* stream);
 
 /*
+ * Host logic of the dispatch, exported for its test (no GPU work): which tile configuration a call takes on a device of
+ * `compute_units`, or -1: no such call.  Dense (G == 0), weight rows x rows of a tile: 0 32x32, 1 64x32, 2 80x32, 3 96x32,
+ * 4 64x64 with two groups of waves along K, 5 64x64, 6 128x128, 7 256x256; grouped: 8 64x32, 9 128x64, 10 64x64, 11 128x128,
+ * 12 256x128, 13 256x256.
+ */
+int ds3_gemm_mxfp4_config(int32_t G, int64_t M, int64_t N, int64_t K, int compute_units);
+
+/*
  * Rows of an expert layer into expert order and back (Section 2.1.2: every token is
  * computed by the top_k experts its router chose).  A choice is a (token, slot).
  *

@@ -40,6 +40,7 @@ SYMBOLS = [
     "ds3_grouped_gemm_workspace_bytes", "ds3_gemm_few_tiles_config", "ds3_gemm_short_k", "ds3_gemm_between_tile", "ds3_gemm_default_kernel", "ds3_gemm_tail_shared",
     "ds3_grouped_gemm_few_rows_tile",
     "ds3_quant_mxfp4", "ds3_quant_mxfp4_t", "ds3_dequant_mxfp4", "ds3_gemm_mxfp4", "ds3_grouped_gemm_mxfp4",
+    "ds3_gemm_mxfp4_config",
     "ds3_moe_sort", "ds3_moe_dispatch", "ds3_moe_dispatch_quant_1x128", "ds3_moe_dispatch_quant_1x128_pow2",
     "ds3_moe_dispatch_quant_mxfp4", "ds3_moe_combine", "ds3_moe_combine_bwd",
 ]
@@ -114,6 +115,7 @@ def _load() -> ctypes.CDLL:
     lib.ds3_dequant_mxfp4.argtypes = [vp, i64, i64, i64, vp, i64, i64, vp, i64, vp]
     lib.ds3_gemm_mxfp4.argtypes = [i64, i64, i64, vp, i64, vp, i64, i64, vp, i64, vp, i64, i64, vp, i32, i64, i32, vp]
     lib.ds3_grouped_gemm_mxfp4.argtypes = [i32, vp, i64, i64, i64, vp, i64, vp, i64, i64, vp, i64, vp, i64, i64, vp, i32, i64, vp]
+    lib.ds3_gemm_mxfp4_config.argtypes = [i32, i64, i64, i64, i32]
     lib.ds3_moe_sort.argtypes = [vp, i64, i32, i64, i32, i32, vp, vp, vp]
     lib.ds3_moe_dispatch.argtypes = [vp, i32, i64, i64, i64, vp, i32, i64, vp, i64, vp]
     for name in ("ds3_moe_dispatch_quant_1x128", "ds3_moe_dispatch_quant_1x128_pow2", "ds3_moe_dispatch_quant_mxfp4"):

@@ -618,6 +618,11 @@ ds3_status ds3_grouped_gemm_mxfp4(int32_t G, const int32_t* group_offsets, int64
                    c, ct, ldc, 0, stream);
 }
 
+int ds3_gemm_mxfp4_config(int32_t G, int64_t M, int64_t N, int64_t K, int compute_units) {
+    if (G < 0 || G > 1023 || M <= 0 || N <= 0 || K <= 0 || K % 128 || M > kMaxDim || N > kMaxDim || K > kMaxDim || compute_units < 8) return -1;
+    return gemm_mxfp4_config(G, (int)M, (int)N, (int)K, compute_units / 8 * 8);
+}
+
 // ---- rows in expert order and back ----------------------------------------------------
 constexpr int kMaxTopK = 64;                                  // one choice a lane
 static ds3_status check_slots(int64_t tokens, int64_t cols, int32_t top_k, int64_t total_rows) {

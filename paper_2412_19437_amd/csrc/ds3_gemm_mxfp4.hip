@@ -34,16 +34,17 @@ struct TileCfg {
     static constexpr int BN = WN * FN * 16, BM = FM * 16;
     static constexpr int ROWS = BN + BM;               // rows of one K-step's codes
     static constexpr int GROUP = ROWS * 128;           // bytes of codes per K-step
-    static constexpr int NSA = (BM + 63) / 64;         // 64-row pieces of the activation scales
-    static constexpr int SCALES = (NSA + 1) * 512;     // per wave and stage: two words an activation row, two a weight row
-    static constexpr int STAGE = WK * GROUP + WN * WK * SCALES;
-    static constexpr int NB = 2 * FN, NA = BM / 8 / WN;         // code loads per thread and stage: weights, activations
-    static constexpr int LOADS = NB + NA + 2 * (NSA + 1);       // vector-memory operations per wave and stage
+    // scale words of a K-step, two a row, in loads of 64: the weight rows', then the activation rows', shared out among the
+    // waves (the last ones fetch the last 64 once more, so that every wave has the same number)
+    static constexpr int LW = (2 * BN + 63) / 64, LA = (2 * BM + 63) / 64, LS = (LW + LA + WN - 1) / WN;
+    static constexpr int GSTAGE = GROUP + (LW + LA) * 256;      // bytes a K-step and wave group
+    static constexpr int STAGE = WK * GSTAGE;
+    static constexpr int NB = 2 * FN, NA = (BM / 8 + WN - 1) / WN;      // code loads per thread and stage: weights, activations
+    static constexpr int LOADS = NB + NA + LS;         // vector-memory operations per wave and stage
     static constexpr int RLD = BN + 4;                 // floats per row of the reduction buffer
     static constexpr int RED = WK * BM * RLD * 4;
     static constexpr int LDS_BYTES = (NS * STAGE > RED ? NS * STAGE : RED);
-    static_assert(FN * 16 <= 64, "one weight row a lane");
-    static_assert(WN % 2 == 0 && (BM / 8) % WN == 0, "load mapping");
+    static_assert(WN % 2 == 0 || (BM / 8) % WN != 0, "load mapping");
     static_assert(NS >= 2 && (NS - 2) * LOADS < 64, "vmcnt immediate");
     static_assert(LDS_BYTES <= 160 * 1024, "LDS");
 };
@@ -131,43 +132,67 @@ __global__ __launch_bounds__(C::NT) void gemm_mxfp4_tile_kernel(const MxGemmPara
     const int gchunk = (lane & 7) ^ swz_key(lrow);
     const unsigned voff_b = (unsigned)(lrow * (int)p.ldb + gchunk * 16), voff_a = (unsigned)(lrow * (int)p.lda + gchunk * 16);
     const unsigned step_b = (unsigned)(8 * WN * (int)p.ldb), step_a = (unsigned)(8 * WN * (int)p.lda);
+    // (an odd number of waves: every other load's rows have the other key; where the activation rows are no whole loads of
+    // all waves, the waves beyond the last eight rows move those once more, the same bytes to the same place)
+    constexpr bool kOdd = WN % 2 != 0, kAgain = (BM / 8) % WN != 0;
+    [[maybe_unused]] const unsigned voff_b1 = (unsigned)(lrow * (int)p.ldb + (gchunk ^ 1) * 16);
+    [[maybe_unused]] int dst_a[C::NA];
+    [[maybe_unused]] unsigned voff_ai[C::NA];
+    if constexpr (kAgain) {
+#pragma unroll
+        for (int i = 0; i < C::NA; ++i) {
+            const int g = min(i * WN + wn, BM / 8 - 1), row = g * 8 + (lane >> 3);
+            dst_a[i] = (BN / 8 + g) * 1024;
+            voff_ai[i] = (unsigned)(row * (int)p.lda + ((lane & 7) ^ swz_key(row)) * 16);
+        }
+    }
     // a half K-step's second half: neither operand's codes are read there (zeros: E2M1 has no value whose product with
     // zero is not zero), and the scales are those of the first half once more
+    // (the keys of a thread's rows differ in their lowest bit only, which leaves a chunk in its half)
     const unsigned past_half = (KW & 1) && gchunk >= 4 ? kOobOffset : 0u;
-    unsigned soff_a[C::NSA];
+    unsigned soff[C::LS], sstep[C::LS];
+    int shalf[C::LS], sdst[C::LS];
+    bool sw_side[C::LS];
 #pragma unroll
-    for (int h = 0; h < C::NSA; ++h) soff_a[h] = (unsigned)(m0 + min(h * 64 + lane, m_rows - 1)) * (unsigned)p.sar * 4u;
-    const unsigned soff_b = (unsigned)(n0 + min(wn * FN * 16 + lane, n_rows - 1)) * (unsigned)p.sbr * 4u;
-    const unsigned sa_step = (unsigned)p.sak * 4u, sb_step = (unsigned)p.sbk * 4u;
+    for (int i = 0; i < C::LS; ++i) {
+        const int l = min(wn + i * WN, C::LW + C::LA - 1);             // wave-uniform
+        sw_side[i] = l < C::LW;
+        const int idx = (sw_side[i] ? l : l - C::LW) * 64 + lane, width = sw_side[i] ? BN : BM;
+        shalf[i] = min(idx / width, 1);
+        const int row = idx - shalf[i] * width;
+        soff[i] = sw_side[i] ? (unsigned)(n0 + min(row, n_rows - 1)) * (unsigned)p.sbr * 4u : (unsigned)(m0 + min(row, m_rows - 1)) * (unsigned)p.sar * 4u;
+        sstep[i] = (unsigned)(sw_side[i] ? p.sbk : p.sak) * 4u;
+        sdst[i] = C::GROUP + l * 256;
+    }
 
-    uint8_t* const codes = smem + wk * C::GROUP;                            // + stage * STAGE
-    uint8_t* const scales = smem + WK * C::GROUP + wave * C::SCALES;        // + stage * STAGE
+    uint8_t* const codes = smem + wk * C::GSTAGE;                           // + stage * STAGE
     auto issue = [&](int step, int stage) {
         const int kb = step * WK + wk;
-        const unsigned koff = (kb < KB ? (unsigned)kb << 7 : kOobOffset);
-        const unsigned more = kb == KB - 1 ? past_half : 0u;
-        uint8_t* dst = codes + stage * C::STAGE + wn * 1024;
+        const unsigned koff = (kb < KB ? (unsigned)kb << 7 : kOobOffset) | (kb == KB - 1 ? past_half : 0u);
+        uint8_t* const base = codes + stage * C::STAGE;
 #pragma unroll
         for (int i = 0; i < C::NB + C::NA; ++i) {
             const bool is_b = i < C::NB;
-            const unsigned voff = ((is_b ? voff_b + (unsigned)i * step_b : voff_a + (unsigned)(i - C::NB) * step_a) + koff) | more;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(is_b ? rs_b : rs_a, (lds_ptr_t)(dst + i * (WN * 1024)), 16, (int)voff, 0, 0, 0);
+            unsigned voff;
+            uint8_t* at = base + wn * 1024 + i * (WN * 1024);
+            if (is_b) voff = (kOdd && i % 2 ? voff_b1 : voff_b) + ((unsigned)i * step_b + koff);
+            else if constexpr (kAgain) {
+                voff = voff_ai[i - C::NB] + koff;
+                at = base + dst_a[i - C::NB];
+            } else voff = voff_a + ((unsigned)(i - C::NB) * step_a + koff);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(is_b ? rs_b : rs_a, (lds_ptr_t)at, 16, (int)voff, 0, 0, 0);
         }
-        uint8_t* sd = scales + stage * C::STAGE;
 #pragma unroll
-        for (int w = 0; w < 2; ++w) {
-            const unsigned kw = (unsigned)min(2 * kb + w, KW - 1);
-#pragma unroll
-            for (int h = 0; h < C::NSA; ++h)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(rs_sa, (lds_ptr_t)(sd + (w * C::NSA + h) * 256), 4, (int)(soff_a[h] + kw * sa_step), 0, 0, 0);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rs_sb, (lds_ptr_t)(sd + (2 * C::NSA + w) * 256), 4, (int)(soff_b + kw * sb_step), 0, 0, 0);
+        for (int i = 0; i < C::LS; ++i) {
+            const unsigned kw = (unsigned)min(2 * kb + shalf[i], KW - 1);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(sw_side[i] ? rs_sb : rs_sa, (lds_ptr_t)(base + sdst[i]), 4, (int)(soff[i] + kw * sstep[i]), 0, 0, 0);
         }
     };
     const int key = swz_key(l16);
     const int foff0 = l16 * 128 + (((2 * g4) ^ key) << 4), foff1 = l16 * 128 + (((2 * g4 + 1) ^ key) << 4);
-    // this lane's two scale bytes of row r: word g4 / 2, bytes 2 * (g4 % 2) and the next
-    const int so_a = (g4 >> 1) * (C::NSA * 256) + (g4 & 1) * 2 + l16 * 4;
-    const int so_b = C::NSA * 512 + (g4 >> 1) * 256 + (g4 & 1) * 2 + l16 * 4;
+    // this lane's two scale bytes of a row: word g4 / 2, bytes 2 * (g4 % 2) and the next
+    const int so_b = C::GROUP + ((g4 >> 1) * BN + wn * FN * 16 + l16) * 4 + (g4 & 1) * 2;
+    const int so_a = C::GROUP + C::LW * 256 + ((g4 >> 1) * BM + l16) * 4 + (g4 & 1) * 2;
 
     const int steps = (KB + WK - 1) / WK;
 #pragma unroll
@@ -188,7 +213,6 @@ __global__ __launch_bounds__(C::NT) void gemm_mxfp4_tile_kernel(const MxGemmPara
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         const uint8_t* st = codes + stage * C::STAGE;
-        const uint8_t* sc = scales + stage * C::STAGE;
         // (everything that is read from LDS in this step is read before the next loads are issued: the
         // compiler makes an LDS read behind LDS-bound loads wait for them)
         i32x4 w[FN][2], x[FM][2];
@@ -198,14 +222,14 @@ __global__ __launch_bounds__(C::NT) void gemm_mxfp4_tile_kernel(const MxGemmPara
             const uint8_t* f = st + (wn * FN + i) * 2048;
             w[i][0] = *reinterpret_cast<const i32x4*>(f + foff0);
             w[i][1] = *reinterpret_cast<const i32x4*>(f + foff1);
-            sw[i] = *reinterpret_cast<const uint16_t*>(sc + so_b + i * 64);
+            sw[i] = *reinterpret_cast<const uint16_t*>(st + so_b + i * 64);
         }
 #pragma unroll
         for (int j = 0; j < FM; ++j) {
             const uint8_t* f = st + (BN + j * 16) * 128;
             x[j][0] = *reinterpret_cast<const i32x4*>(f + foff0);
             x[j][1] = *reinterpret_cast<const i32x4*>(f + foff1);
-            sx[j] = *reinterpret_cast<const uint16_t*>(sc + so_a + j * 64);
+            sx[j] = *reinterpret_cast<const uint16_t*>(st + so_a + j * 64);
         }
         __builtin_amdgcn_sched_barrier(0);
         issue(s + NS - 1, stage == 0 ? NS - 1 : stage - 1);
@@ -282,9 +306,7 @@ struct MainCfg {
     static constexpr int LDS_BYTES = NS * (STAGE + SSTAGE) + (kMaxExperts + 1) * 4;
     static constexpr int WG_PER_CU = NT > 256 || LDS_BYTES > 80 * 1024 ? 1 : 2;
     static_assert(BN % RPI == 0 && BM % RPI == 0 && RPI % 16 == 0, "load mapping");
-    static constexpr int SR = (ROWS + NT - 1) / NT;    // rows of scales a thread fetches
-    static_assert(BN % 64 == 0 && BM % 64 == 0, "a wave fetches scales of one side");
-    static_assert(SR == 1 || (SR == 2 && BN == NT && BM == NT), "one row of scales a thread, or one of each side");
+    static_assert(BN % 64 == 0 && BM % 64 == 0 && ROWS <= NT, "a thread fetches one row's scales, a wave those of one side");
     static_assert(FM % 2 == 0 && HEADN <= NSUB - FN && LPT <= 2 * FN, "loads are interleaved with the matrix instructions");
     static_assert((NT / 64) * 16 * (TN * 4 + 16) <= STAGE, "epilogue strips take the last stage");
     static_assert(LDS_BYTES <= 160 * 1024, "LDS");
@@ -292,8 +314,8 @@ struct MainCfg {
 
 struct MxTile {
     int m0, n0, m_rows, n_rows;
-    __amdgpu_buffer_rsrc_t rs_a, rs_b, rs_s[2];
-    unsigned s_off[2];         // byte offsets of the rows of scales this thread fetches from
+    __amdgpu_buffer_rsrc_t rs_a, rs_b, rs_s;
+    unsigned s_off;            // byte offset of the row of scales this thread fetches from
 };
 
 // Persistent workgroups; XCD x (workgroups are dealt to the eight of them in turn) walks its eighth of the tile list.  The
@@ -302,7 +324,7 @@ struct MxTile {
 // next K-step's first fragments, under the last fragment's matrix instructions.
 template <class C, bool OUT_BF16, bool GROUPED>
 __global__ __launch_bounds__(C::NT) void gemm_mxfp4_kernel(const MxGemmParams p) {
-    constexpr int BN = C::BN, BM = C::BM, NT = C::NT, NS = C::NS, FN = C::FN, FM = C::FM, STAGE = C::STAGE, NSUB = C::NSUB;
+    constexpr int BN = C::BN, BM = C::BM, NT = C::NT, NS = C::NS, FN = C::FN, FM = C::FM, STAGE = C::STAGE;
     __shared__ __attribute__((aligned(1024))) uint8_t smem[C::LDS_BYTES];
     uint8_t* const scales = smem + NS * STAGE;
     int* const before = reinterpret_cast<int*>(scales + NS * C::SSTAGE);       // [G + 1] row tiles before expert g
@@ -388,16 +410,12 @@ __global__ __launch_bounds__(C::NT) void gemm_mxfp4_kernel(const MxGemmParams p)
         c.rs_a = __builtin_amdgcn_make_buffer_rsrc((void*)(p.a + (int64_t)m0 * p.lda), 0, (int)((int64_t)(c.m_rows - 1) * p.lda + kbytes), 0x00020000);
         c.rs_b = __builtin_amdgcn_make_buffer_rsrc((void*)(p.b + (int64_t)grp * p.b_group_stride + (int64_t)n0 * p.ldb), 0,
                                                    (int)((int64_t)(c.n_rows - 1) * p.ldb + kbytes), 0x00020000);
-        // Thread t fetches the scales of tile row t (weight rows first) and, where there are more rows than threads, of
-        // row t + NT (rows past the valid ones repeat the last; all offsets are valid, the range check is not relied on).
-#pragma unroll
-        for (int r = 0; r < C::SR; ++r) {
-            const bool w_side = r * NT + wave * 64 < BN;
-            const int row = r * NT + tid;
-            c.rs_s[r] = __builtin_amdgcn_make_buffer_rsrc((void*)(w_side ? p.sb + (int64_t)grp * p.sb_group_stride : p.sa), 0, 0x7ffffffc, 0x00020000);
-            c.s_off[r] = w_side ? (unsigned)(n0 + min(row, c.n_rows - 1)) * (unsigned)p.sbr * 4u
-                                : (unsigned)(m0 + min(max(row - BN, 0), c.m_rows - 1)) * (unsigned)p.sar * 4u;
-        }
+        // Thread t fetches the scales of tile row t, weight rows first (rows past the valid ones repeat the last; all
+        // offsets are valid, the range check is not relied on).
+        const bool w_side = wave * 64 < BN;
+        c.rs_s = __builtin_amdgcn_make_buffer_rsrc((void*)(w_side ? p.sb + (int64_t)grp * p.sb_group_stride : p.sa), 0, 0x7ffffffc, 0x00020000);
+        c.s_off = w_side ? (unsigned)(n0 + min(tid, c.n_rows - 1)) * (unsigned)p.sbr * 4u
+                         : (unsigned)(m0 + min(max(tid - BN, 0), c.m_rows - 1)) * (unsigned)p.sar * 4u;
         return true;
     };
 
@@ -414,10 +432,10 @@ __global__ __launch_bounds__(C::NT) void gemm_mxfp4_kernel(const MxGemmParams p)
     // this lane's two scale bytes: word g4 / 2 of its row, bytes 2 * (g4 % 2) and the next
     const int so = (g4 >> 1) * (C::SROW * 4) + (g4 & 1) * 2 + l16 * 4;
     const int ps_base = so + wn * C::TN * 4, qs_base = so + (BN + wm * C::TM) * 4;
-    const bool scale_role = C::SR == 2 || wave * 64 < C::ROWS;
-    // (in vector registers: as scalars they would be re-read from the kernel arguments inside the K-loop)
-    unsigned sc_kstride[2] = {(unsigned)(wave * 64 < BN ? (int)p.sbk : (int)p.sak) * 4u, (unsigned)(int)p.sak * 4u};
-    asm volatile("" : "+v"(sc_kstride[0]), "+v"(sc_kstride[1]));
+    const bool scale_role = wave * 64 < C::ROWS;
+    // (in a vector register: as a scalar it would be re-read from the kernel arguments inside the K-loop)
+    unsigned sc_kstride = (unsigned)(wave * 64 < BN ? (int)p.sbk : (int)p.sak) * 4u;
+    asm volatile("" : "+v"(sc_kstride));
 
     // byte offset of K-step kb for this thread's loads (out of range beyond the last)
     auto koff_of = [&](int kb) -> unsigned {
@@ -438,10 +456,8 @@ __global__ __launch_bounds__(C::NT) void gemm_mxfp4_kernel(const MxGemmParams p)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const unsigned kw = (unsigned)min(2 * kb + h, KW - 1);
-#pragma unroll
-            for (int r = 0; r < C::SR; ++r)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(c.rs_s[r], (lds_ptr_t)(scales + stage * C::SSTAGE + (h * C::SROW + r * NT + wave * 64) * 4), 4,
-                                                         (int)(c.s_off[r] + kw * sc_kstride[r]), 0, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(c.rs_s, (lds_ptr_t)(scales + stage * C::SSTAGE + (h * C::SROW + wave * 64) * 4), 4,
+                                                     (int)(c.s_off + kw * sc_kstride), 0, 0, 0);
         }
     };
     struct Frag { i32x4 h0, h1; };
@@ -460,7 +476,7 @@ __global__ __launch_bounds__(C::NT) void gemm_mxfp4_kernel(const MxGemmParams p)
     };
     auto kstep_barrier = [&]() {
         if constexpr (NS == 2) barrier_keep(std::integral_constant<int, 0>{});
-        else if (scale_role) barrier_keep(std::integral_constant<int, C::LPT + 2 * C::SR>{});
+        else if (scale_role) barrier_keep(std::integral_constant<int, C::LPT + 2>{});
         else barrier_keep(std::integral_constant<int, C::LPT>{});
     };
     auto issue_first_steps = [&](const MxTile& c) {
@@ -672,25 +688,18 @@ __global__ __launch_bounds__(C::NT) void gemm_mxfp4_kernel(const MxGemmParams p)
 }
 
 // ---- host side -------------------------------------------------------------------
-template <class C>
+template <class C, bool GROUPED>
 static ds3_status launch_tile(MxGemmParams p, ds3_dtype ct, hipStream_t st) {
     p.tiles_m = (p.M + C::BM - 1) / C::BM;
-    if (p.G > 0) {
-        // an upper bound (a row tile has a row); workgroups beyond the true count leave at once
-        p.tiles_m = (int)std::min<int64_t>((int64_t)p.tiles_m + p.G, p.M);
-    }
+    // grouped: an upper bound (a row tile has a row); workgroups beyond the true count leave at once
+    if (GROUPED) p.tiles_m = (int)std::min<int64_t>((int64_t)p.tiles_m + p.G, p.M);
     p.tiles_n = (p.N + C::BN - 1) / C::BN;
     const int64_t n = ((int64_t)p.tiles_m * p.tiles_n + 7) / 8 * 8;
     if (n * C::NT >= (1ll << 32)) return DS3_ERR_UNSUPPORTED;
     const dim3 grid((unsigned)n), block(C::NT);
     (void)hipGetLastError();                            // a stale error of earlier, unrelated work is not this launch's
-    if (p.G > 0) {
-        if (ct == DS3_BF16) gemm_mxfp4_tile_kernel<C, true, true><<<grid, block, 0, st>>>(p);
-        else gemm_mxfp4_tile_kernel<C, false, true><<<grid, block, 0, st>>>(p);
-    } else {
-        if (ct == DS3_BF16) gemm_mxfp4_tile_kernel<C, true, false><<<grid, block, 0, st>>>(p);
-        else gemm_mxfp4_tile_kernel<C, false, false><<<grid, block, 0, st>>>(p);
-    }
+    if (ct == DS3_BF16) gemm_mxfp4_tile_kernel<C, true, GROUPED><<<grid, block, 0, st>>>(p);
+    else gemm_mxfp4_tile_kernel<C, false, GROUPED><<<grid, block, 0, st>>>(p);
     return hipGetLastError() == hipSuccess ? DS3_OK : DS3_ERR_LAUNCH;
 }
 
@@ -701,34 +710,100 @@ static int compute_units_x8() {
     return n / 8 * 8;
 }
 
-template <class C>
+template <class C, bool GROUPED>
 static ds3_status launch_main(MxGemmParams p, ds3_dtype ct, int cus, hipStream_t st) {
     p.tiles_m = (p.M + C::BM - 1) / C::BM;
-    if (p.G > 0) p.tiles_m = (int)std::min<int64_t>((int64_t)p.tiles_m + p.G, p.M);     // (an upper bound)
+    if (GROUPED) p.tiles_m = (int)std::min<int64_t>((int64_t)p.tiles_m + p.G, p.M);     // (an upper bound)
     p.tiles_n = (p.N + C::BN - 1) / C::BN;
     const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n, want = (tiles + 7) / 8 * 8, slots = (int64_t)cus * C::WG_PER_CU;
     if (tiles > (1ll << 31) - 16) return DS3_ERR_UNSUPPORTED;
     const dim3 grid((unsigned)std::min(want, slots)), block(C::NT);
     (void)hipGetLastError();                            // a stale error of earlier, unrelated work is not this launch's
-    if (p.G > 0) {
-        if (ct == DS3_BF16) gemm_mxfp4_kernel<C, true, true><<<grid, block, 0, st>>>(p);
-        else gemm_mxfp4_kernel<C, false, true><<<grid, block, 0, st>>>(p);
-    } else {
-        if (ct == DS3_BF16) gemm_mxfp4_kernel<C, true, false><<<grid, block, 0, st>>>(p);
-        else gemm_mxfp4_kernel<C, false, false><<<grid, block, 0, st>>>(p);
-    }
+    if (ct == DS3_BF16) gemm_mxfp4_kernel<C, true, GROUPED><<<grid, block, 0, st>>>(p);
+    else gemm_mxfp4_kernel<C, false, GROUPED><<<grid, block, 0, st>>>(p);
     return hipGetLastError() == hipSuccess ? DS3_OK : DS3_ERR_LAUNCH;
+}
+
+// The configurations and what a call takes with each: `fixed` + one round of tiles after another, a round being K-steps
+// (of 256) / `wk` steps of `full` us when every workgroup slot has a tile and `alone` us when few have, plus the sums' way
+// out.  Fitted to 9000 shapes (M 1 .. 4096, N 64 .. 24576, K 128 .. 18432, weights from HBM, BF16 output); on 7700 others
+// the one it picks takes 1.030 of the best of 17 configurations' time on average (the best of these eight 1.014), one call
+// in ten more than 1.1 of it, most of those of 5 us, which repeat to 10%.
+struct MxChoice { int bn, bm, wk, per_cu; float fixed, full, alone, out; };
+enum { kMx32x32, kMx64x32, kMx80x32, kMx96x32, kMx64x64two, kMx64x64, kMx128x128, kMx256x256, kMxCfgs };
+constexpr MxChoice kMx[kMxCfgs] = {
+    {32, 32, 4, 1, 2.80f, 0.496f, 0.259f, 1.04f},   {64, 32, 2, 2, 2.69f, 0.660f, 0.244f, 1.38f},
+    {80, 32, 2, 1, 2.50f, 0.487f, 0.321f, 1.59f},   {96, 32, 2, 1, 2.49f, 0.520f, 0.340f, 1.55f},
+    {64, 64, 2, 1, 2.35f, 0.580f, 0.410f, 1.62f},   {64, 64, 1, 2, 2.23f, 0.488f, 0.246f, 1.84f},
+    {128, 128, 1, 2, 1.87f, 1.210f, 0.417f, 2.62f}, {256, 256, 1, 1, 0.00f, 2.017f, 0.798f, 5.64f},
+};
+static double mx_time(const MxChoice& c, int64_t tiles_m, int N, int K, int cus) {
+    const int64_t tiles = tiles_m * ((N + c.bn - 1) / c.bn), slots = (int64_t)cus * c.per_cu, rest = tiles % slots;
+    const double steps = ((K + 255) / 256 + c.wk - 1) / c.wk, part = (double)rest / (double)slots;
+    double us = c.fixed + (double)(tiles / slots) * (steps * c.full + c.out);
+    if (rest) us += steps * (c.alone + (c.full - c.alone) * part) + c.out;
+    return us;
+}
+static int mx_dense_choice(int M, int N, int K, int cus) {
+    int best = kMx256x256;
+    double best_us = 0.;
+    for (int i = kMxCfgs - 1; i >= 0; --i) {
+        const MxChoice& c = kMx[i];
+        if (c.wk > (K + 255) / 256) continue;          // (groups of waves without a K-step)
+        const int64_t tiles_m = (M + c.bm - 1) / c.bm;
+        // (a grid of a workgroup a tile: far beyond where these are the fastest)
+        if (i < kMx128x128 && tiles_m * ((N + c.bn - 1) / c.bn) > (1 << 20)) continue;
+        const double us = mx_time(c, tiles_m, N, K, cus);
+        if (i == kMx256x256 || us < best_us) { best = i; best_us = us; }
+    }
+    return best;
+}
+
+// Grouped: by the mean rows of an expert (the host knows no more).  Weights from HBM, us with 64x32 / 128x64 / 128x128 /
+// 256x128 / 256x256 tiles: 32 experts of 4 rows, N 7168, K 2048 46 / 49 / - / - / -; of 32, N 4096, K 7168 113 / 93 / - / - /
+// -; of 64 - / 122 / 97 / 94 / 106; of 128 - / 158 / 148 / 137 / 119; of 256 - / 236 / 194 / 174 / 172; 8 experts of 512 - /
+// 111 / 101 / 92 / 98; N 7168, K 2048, 32 experts of 64 - / 68 / 59 / 61 / 68, of 256 - / 158 / 124 / 114 / 111.
+// Few tiles (8 experts of 128 rows, N 2048, K 1024): 64x64 9.2, 128x128 7.6, 256x256 11.4.
+enum { kMxG64x32, kMxG128x64, kMxG64x64, kMxG128x128, kMxG256x128, kMxG256x256 };
+static int mx_grouped_choice(int G, int M, int N, int K, int cus) {
+    const int64_t mean = ((int64_t)M + G - 1) / G;
+    if (mean <= 24) return kMxG64x32;
+    if (mean <= 48) return kMxG128x64;
+    const int most = mean > 96 && mean <= 256 ? kMxG256x256 : kMxG256x128;
+    auto tiles_m = [&](int bm) { return (int64_t)M / bm + (G + 1) / 2; };      // (half a tile an expert is lost on average)
+    if (tiles_m(most == kMxG256x256 ? 256 : 128) * ((N + 255) / 256) * 4 >= 3 * (int64_t)cus) return most;
+    const double t64 = mx_time(kMx[kMx64x64], tiles_m(64), N, K, cus), t128 = mx_time(kMx[kMx128x128], tiles_m(128), N, K, cus);
+    return t64 < t128 ? kMxG64x64 : kMxG128x128;
+}
+
+int gemm_mxfp4_config(int G, int M, int N, int K, int cus) {
+    return G > 0 ? kMxCfgs + mx_grouped_choice(G, M, N, K, cus) : mx_dense_choice(M, N, K, cus);
 }
 
 ds3_status launch_gemm_mxfp4(const MxGemmParams& p, ds3_dtype ct, hipStream_t st) {
     // 32-bit offsets inside a tile of up to 256 rows
     if ((int64_t)257 * p.ldb + p.K / 2 >= (1ll << 31) || (int64_t)257 * p.lda + p.K / 2 >= (1ll << 31)) return DS3_ERR_UNSUPPORTED;
     const int cus = compute_units_x8();
-    const int64_t rows = p.G > 0 ? (p.M + p.G - 1) / p.G : p.M;
-    if (p.G == 0 && (int64_t)((p.M + 255) / 256) * ((p.N + 255) / 256) * 8 >= 5 * (int64_t)cus) return launch_main<MainCfg<256, 256, 4, 2, 2>>(p, ct, cus, st);
-    if (p.G > 0 && rows > 64) return launch_main<MainCfg<256, 128, 4, 2, 3>>(p, ct, cus, st);
-    if (rows <= 32) return launch_tile<TileCfg<2, 2, 4, 1, 3>>(p, ct, st);
-    return launch_tile<TileCfg<2, 8, 4, 1, 3>>(p, ct, st);
+    if (p.G > 0) {
+        switch (mx_grouped_choice(p.G, p.M, p.N, p.K, cus)) {
+            case kMxG64x32: return launch_tile<TileCfg<1, 2, 4, 1, 3>, true>(p, ct, st);
+            case kMxG128x64: return launch_tile<TileCfg<2, 4, 4, 1, 3>, true>(p, ct, st);
+            case kMxG64x64: return launch_tile<TileCfg<1, 4, 4, 1, 4>, true>(p, ct, st);
+            case kMxG128x128: return launch_main<MainCfg<128, 128, 2, 2, 2>, true>(p, ct, cus, st);
+            case kMxG256x128: return launch_main<MainCfg<256, 128, 4, 2, 3>, true>(p, ct, cus, st);
+            default: return launch_main<MainCfg<256, 256, 4, 2, 2>, true>(p, ct, cus, st);
+        }
+    }
+    switch (mx_dense_choice(p.M, p.N, p.K, cus)) {
+        case kMx32x32: return launch_tile<TileCfg<1, 2, 2, 4, 3>, false>(p, ct, st);
+        case kMx64x32: return launch_tile<TileCfg<1, 2, 4, 2, 3>, false>(p, ct, st);
+        case kMx80x32: return launch_tile<TileCfg<1, 2, 5, 2, 4>, false>(p, ct, st);
+        case kMx96x32: return launch_tile<TileCfg<1, 2, 6, 2, 3>, false>(p, ct, st);
+        case kMx64x64two: return launch_tile<TileCfg<1, 4, 4, 2, 3>, false>(p, ct, st);
+        case kMx64x64: return launch_tile<TileCfg<1, 4, 4, 1, 4>, false>(p, ct, st);
+        case kMx128x128: return launch_main<MainCfg<128, 128, 2, 2, 2>, false>(p, ct, cus, st);
+        default: return launch_main<MainCfg<256, 256, 4, 2, 2>, false>(p, ct, cus, st);
+    }
 }
 
 }  // namespace ds3

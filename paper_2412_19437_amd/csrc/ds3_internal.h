@@ -135,6 +135,8 @@ struct MxGemmParams {
     int accumulate;
 };
 ds3_status launch_gemm_mxfp4(const MxGemmParams& p, ds3_dtype ct, hipStream_t st);
+// Which configuration a call takes (ds3_gemm_mxfp4_config's values).
+int gemm_mxfp4_config(int G, int M, int N, int K, int cus);
 
 // ---- rows in expert order and back ----------------------------------------------------
 ds3_status launch_moe_sort(const int32_t* ids, int64_t tokens, int top_k, int64_t ld, int first, int G, int32_t* offsets,

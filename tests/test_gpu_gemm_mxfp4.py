@@ -58,6 +58,68 @@ def test_dense(ds3, M, N, K):
     assert (c[:, N:] == 3.0).all()
 
 
+def compute_units():
+    return torch.cuda.get_device_properties(0).multi_processor_count
+
+
+# a shape (or several) for every tile configuration of the dense call, with ragged edges and K-steps that end in a half
+DENSE = {0: [(20, 1500, 2688)], 1: [(30, 12000, 1408), (120, 4001, 2176)], 2: [(16, 18431, 7168), (3529, 67, 640)],
+         3: [(9, 24001, 2176), (300, 2100, 1920)], 4: [(450, 2001, 896), (4451, 33, 384)], 5: [(333, 4001, 640)],
+         6: [(65, 16794, 384), (2048, 2304, 896)], 7: [(5000, 9216, 384), (265, 21812, 384)]}
+
+
+@pytest.mark.parametrize("config", sorted(DENSE))
+def test_every_dense_configuration(ds3, config):
+    for M, N, K in DENSE[config]:
+        announce(f"mxfp4 gemm {M}x{N}x{K}, configuration {config}")
+        assert compute_units() != 256 or ds3._L().ds3_gemm_mxfp4_config(0, M, N, K, 256) == config
+        rng = np.random.default_rng(config)
+        a, qa, sa = operand(rng, M, K, lead=1)
+        b, qb, sb = operand(rng, N, K, lead=2)
+        da, db = torch.from_numpy(a).to(DEV), torch.from_numpy(b).to(DEV)      # (the products in 64 bits on the device: large)
+        want, mag = da @ db.t(), da.abs() @ db.abs().t()
+        near = (K / 128 + 4) * 2.0 ** -23 * mag
+        y = ds3.ds3_gemm_mxfp4(qa, words(sa), qb, words(sb), out_dtype=torch.float32)
+        assert bool(((y.double() - want).abs() <= near).all())
+        y = ds3.ds3_gemm_mxfp4(qa, words(sa, False), qb, words(sb))
+        assert bool(((y.double() - want).abs() <= near + 2.0 ** -8 * (want.abs() + near)).all())
+        c = torch.full((M, (N + 3) // 4 * 4 + 4), -2.0, device=DEV)
+        ds3.ds3_gemm_mxfp4(qa, words(sa), qb, words(sb), c=c[:, :N], accumulate=True)
+        assert bool(((c[:, :N].double() + 2 - want).abs() <= near + 2.0 ** -23 * (want.abs() + 2)).all()) and bool((c[:, N:] == -2).all())
+
+
+# experts' rows (with some empty, some uneven), N, K for every configuration of the grouped call
+GROUPED = {8: ((3, 0, 40, 1, 17, 0, 2, 8), 300, 896), 9: ((40, 0, 33, 60, 31, 47, 1, 100), 260, 640), 10: ((70, 0, 55, 130, 64, 60, 80, 50), 264, 2688),
+           11: ((120, 90, 0, 200, 64, 65, 129, 300), 2056, 384), 12: ((60, 0, 129, 90, 64, 257, 31, 1) * 4, 4104, 384),
+           13: ((250, 100, 0, 300, 257, 129, 1, 256) * 4, 4104, 384)}
+
+
+@pytest.mark.parametrize("config", sorted(GROUPED))
+def test_every_grouped_configuration(ds3, config):
+    sizes, N, K = GROUPED[config]
+    G, rows = len(sizes), sum(sizes) + 5
+    announce(f"mxfp4 grouped {G} experts, {rows} rows, {N}x{K}, configuration {config}")
+    assert compute_units() != 256 or ds3._L().ds3_gemm_mxfp4_config(G, rows, N, K, 256) == config
+    rng = np.random.default_rng(config)
+    off = np.concatenate([[0], np.cumsum(sizes)]).astype(np.int32)
+    a, qa, sa = operand(rng, rows, K, lead=1)
+    b, qb, sb = operand(rng, G * N, K)
+    w = words(sb, False).view(G, N, K // 128).transpose(1, 2).contiguous().transpose(1, 2)
+    qb = qb.contiguous().view(G, N, K // 2)
+    offd = torch.from_numpy(off).to(DEV)
+    for dtype in (torch.float32, torch.bfloat16):
+        c = torch.full((rows, (N + 7) // 8 * 8), 5.0, dtype=dtype, device=DEV)
+        y = ds3.ds3_grouped_gemm_mxfp4(qa, words(sa), offd, qb, w, c=c[:, :N])
+        assert bool((c[:, N:] == 5).all()) and bool((y[off[-1] :] == 5).all())
+        for g in range(G):
+            at = slice(int(off[g]), int(off[g + 1]))
+            da, db = torch.from_numpy(a[at]).to(DEV), torch.from_numpy(b[g * N : (g + 1) * N]).to(DEV)
+            want = da @ db.t()
+            near = (K / 128 + 4) * 2.0 ** -23 * (da.abs() @ db.abs().t())
+            tol = near + 2.0 ** -8 * (want.abs() + near) if dtype == torch.bfloat16 else near
+            assert bool(((y[at].double() - want).abs() <= tol).all())
+
+
 @pytest.mark.parametrize("M,N,K", [(5, 40, 256), (48, 96, 384), (130, 260, 1024), (512, 512, 896)])
 def test_equal_scales_are_exact(ds3, M, N, K):
     """With one scale everything is a multiple of 1/4 below 2^22: FP32 sums in any order are exact."""

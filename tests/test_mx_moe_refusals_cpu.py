@@ -82,6 +82,18 @@ def test_products(pkg, mem):
     assert _try(fn, good, G=1023, N=1 << 24, ldb=128, ldc=1 << 24, sbk=1 << 24) == UNSUPPORTED
 
 
+def test_configuration_query(pkg):
+    f = pkg._L().ds3_gemm_mxfp4_config
+    for bad in ((0, 0, 64, 128, 256), (0, 16, 0, 128, 256), (0, 16, 64, 0, 256), (0, 16, 64, 100, 256), (0, 16, 64, 128, 4), (-1, 16, 64, 128, 256),
+                (1024, 16, 64, 128, 256), (0, 1 << 31, 64, 128, 256)):
+        assert f(*bad) == -1
+    seen = {f(0, m, n, k, 256) for m in (1, 16, 100, 450, 2048, 4096) for n in (576, 2001, 18432) for k in (128, 896, 2176, 7168)}
+    seen |= {f(0, 333, 4001, 640, 256)} | {f(8, 8 * m, n, 384, 256) for m in (4, 40, 60, 128, 200, 600) for n in (64, 264, 2056, 8192)}
+    assert seen == set(range(14))
+    # the groups of waves of a tile never outnumber the K-steps of 256
+    assert f(0, 1, 512, 128, 256) == 5 and f(0, 1, 512, 512, 256) != 0
+
+
 def test_expert_order(pkg, mem):
     L = pkg._L()
     good = dict(ids=mem, tokens=8, k=2, ld=2, first=0, G=4, off=mem, rows=mem, st=None)
