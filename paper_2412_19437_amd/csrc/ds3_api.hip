@@ -627,7 +627,7 @@ int ds3_gemm_mxfp4_config(int32_t G, int64_t M, int64_t N, int64_t K, int comput
 constexpr int kMaxTopK = 64;                                  // one choice a lane
 static ds3_status check_slots(int64_t tokens, int64_t cols, int32_t top_k, int64_t total_rows) {
     if (tokens < 0 || cols < 0 || top_k < 1 || total_rows < 0) return DS3_ERR_SHAPE;
-    if (top_k > kMaxTopK || tokens > kMaxDim / top_k || cols > kMaxDim || total_rows > kMaxDim) return DS3_ERR_UNSUPPORTED;
+    if (top_k > kMaxTopK || tokens > (kMaxDim - 8191) / top_k || cols > kMaxDim || total_rows > kMaxDim) return DS3_ERR_UNSUPPORTED;
     return DS3_OK;
 }
 

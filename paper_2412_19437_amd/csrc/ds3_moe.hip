@@ -46,43 +46,68 @@ __device__ __forceinline__ int block_exclusive(int v, int* part) {
     if (lane == 63) part[wave] = sum;
     __syncthreads();
     int before = 0;
-    for (int w = 0; w < wave; ++w) before += part[w];
+#pragma unroll
+    for (int w = 0; w < kSortThreads / 64; ++w) before += w < wave ? part[w] : 0;
     return before + sum - v;
 }
 
-// Places choices [i0, i1) (at most kSortChunk) in order: base[g] is the next free row of expert g.  Within a wave the
-// lanes of the same expert find each other by a ballot per bit of its number; the waves take turns.
+// Places choices [i0, i1) in order: base[g] is the next free row of expert g, e the expert of choice i0 + tid.  Within a
+// wave the lanes of the same expert find each other by a ballot per bit of its number; the waves leave their counts, a byte
+// each, in the expert's row of `waves` (zeros before and after), where each sums up those of the waves before it.
+struct SortShared {
+    int base[kSortMaxGroups + 1];
+    u32x4 waves[kSortMaxGroups + 1];
+    int part[kSortThreads / 64];
+};
+__device__ __forceinline__ int byte_sum(unsigned int v, int acc) { return (int)__builtin_amdgcn_sad_u8(v, 0u, (unsigned int)acc); }
 template <bool PACKED>
-__device__ __forceinline__ void place(const SortParams& p, int i0, int i1, int* base) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+__device__ __forceinline__ void place(const SortParams& p, int i0, int i1, int e, SortShared& s) {
+    static_assert(kSortThreads == 64 * 16, "a byte a wave");
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int bits = 32 - __clz(p.G);
     for (int at = i0; at < i1; at += kSortThreads) {
-        const int i = at + (int)threadIdx.x;
-        const int e = i < i1 ? sort_expert<PACKED>(p, i) : -1;
+        const int i = at + tid;
+        if (at != i0) e = i < i1 ? sort_expert<PACKED>(p, i) : -1;
         unsigned long long same = __ballot(e >= 0);
         for (int b = 0; b < bits; ++b) {
             const unsigned long long set = __ballot((e >> b) & 1);
             same &= ((e >> b) & 1) ? set : ~set;
         }
         const int rank = __popcll(same & ((1ull << lane) - 1));
+        if (e >= 0 && rank == 0) reinterpret_cast<uint8_t*>(&s.waves[e])[wave] = (uint8_t)__popcll(same);
+        __syncthreads();
         int row = -1;
-        const int waves = min(kSortThreads, i1 - at + 63) >> 6;
-        for (int w = 0; w < waves; ++w) {
-            if (wave == w && e >= 0) {
-                row = base[e] + rank;
-                if (rank == 0) base[e] = row + __popcll(same);
+        if (e >= 0) {
+            const u32x4 w = s.waves[e];
+            int n = s.base[e] + rank;
+            // the bytes of waves 0 .. wave - 1
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int k = wave - 4 * q;
+                n = byte_sum(k >= 4 ? w[q] : k > 0 ? w[q] & ((1u << (8 * k)) - 1) : 0u, n);
             }
-            __syncthreads();
+            row = n;
         }
         if (i < i1) p.rows[i] = row;
+        if (at + kSortThreads < i1) {
+            __syncthreads();
+            const u32x4 w = s.waves[tid];
+            s.base[tid] += byte_sum(w.x, byte_sum(w.y, byte_sum(w.z, byte_sum(w.w, 0))));
+            s.waves[tid] = u32x4{0u, 0u, 0u, 0u};
+            __syncthreads();
+        }
     }
 }
 
 // One launch: every workgroup counts all choices, those before its own 1024 apart, so none waits for another.
 template <bool PACKED>
 __global__ __launch_bounds__(kSortThreads) void moe_sort_kernel(const SortParams p) {
-    __shared__ int before[kSortMaxGroups + 1], total[kSortMaxGroups + 1], part[kSortThreads / 64];
+    __shared__ SortShared s;
+    __shared__ int total[kSortMaxGroups + 1];
+    int* const before = s.base;
     const int tid = threadIdx.x, start = (int)blockIdx.x * kSortThreads;
+    const int own = start + tid < p.n ? sort_expert<PACKED>(p, start + tid) : -1;      // (fetched while the others are counted)
+    s.waves[tid] = u32x4{0u, 0u, 0u, 0u};
     before[tid] = 0;
     total[tid] = 0;
     // few experts: several copies of each count, a lane's own, or the lanes of a wave wait for each other (65536 choices
@@ -134,11 +159,11 @@ __global__ __launch_bounds__(kSortThreads) void moe_sort_kernel(const SortParams
         }
         all += mine;
     }
-    const int off = block_exclusive(all, part);        // (its barrier: the copies are summed before the sums replace them)
+    const int off = block_exclusive(all, s.part);      // (its barrier: the copies are summed before the sums replace them)
     if (tid < p.G) before[tid] = mine + off;
     if (blockIdx.x == 0 && tid <= p.G) p.offsets[tid] = off;     // (thread G holds no expert: the sum of all)
     __syncthreads();
-    place<PACKED>(p, start, min(start + kSortThreads, p.n), before);
+    place<PACKED>(p, start, min(start + kSortThreads, p.n), own, s);
 }
 
 // The long form, for more choices than each workgroup should count: chunks are counted, the counts summed up over the
@@ -186,8 +211,11 @@ __global__ __launch_bounds__(kSortThreads) void moe_sort_scan_kernel(const SortP
 }
 template <bool PACKED>
 __global__ __launch_bounds__(kSortThreads) void moe_sort_place_kernel(const SortParams p, int chunks) {
-    __shared__ int base[kSortMaxGroups + 1];
-    const int tid = threadIdx.x, chunk = blockIdx.x;
+    __shared__ SortShared s;
+    int* const base = s.base;
+    const int tid = threadIdx.x, chunk = blockIdx.x, start = chunk * kSortChunk;
+    const int own = start + tid < p.n ? sort_expert<PACKED>(p, start + tid) : -1;
+    s.waves[tid] = u32x4{0u, 0u, 0u, 0u};
     if (chunk == chunks - 1) {
         count_chunk<PACKED>(p, chunk, base);
         if (tid < p.G) base[tid] = p.offsets[tid + 1] - base[tid];
@@ -195,7 +223,7 @@ __global__ __launch_bounds__(kSortThreads) void moe_sort_place_kernel(const Sort
         base[tid] = p.offsets[tid] + p.rows[(int64_t)chunk * kSortChunk + tid];
     }
     __syncthreads();                                   // (the counts are read before the first rows are written over them)
-    place<PACKED>(p, chunk * kSortChunk, min((chunk + 1) * kSortChunk, p.n), base);
+    place<PACKED>(p, start, min(start + kSortChunk, p.n), own, s);
 }
 
 // =============================================================================
@@ -206,15 +234,20 @@ __device__ __forceinline__ unsigned long long token_rows(const int32_t* rows, in
     return __ballot(row >= 0 && row < total_rows);
 }
 
-// Eight columns of a row.
-template <typename T> __device__ __forceinline__ void store8(uint8_t* p, const float* v, int64_t left);
-template <> __device__ __forceinline__ void store8<Bf16>(uint8_t* p, const float* v, int64_t left) {
-    if (left > 0)
-        *reinterpret_cast<u32x4*>(p) = u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+// Eight columns of a row.  NT: with the non-temporal hint (a template parameter: of the two stores behind a branch the
+// compiler makes one, without the hint).
+template <bool NT, typename V> __device__ __forceinline__ void store16(uint8_t* p, V v) {
+    if constexpr (NT) st_nt(p, v);
+    else st_stream(p, v);
 }
-template <> __device__ __forceinline__ void store8<F32>(uint8_t* p, const float* v, int64_t left) {
-    if (left > 0) *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
-    if (left > 4) *reinterpret_cast<f32x4*>(p + 16) = f32x4{v[4], v[5], v[6], v[7]};
+template <typename T, bool NT> __device__ __forceinline__ void store8(uint8_t* p, const float* v, int64_t left) {
+    if constexpr (T::EPL == 8) {
+        if (left > 0)
+            store16<NT>(p, u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])});
+    } else {
+        if (left > 0) store16<NT>(p, f32x4{v[0], v[1], v[2], v[3]});
+        if (left > 4) store16<NT>(p + 16, f32x4{v[4], v[5], v[6], v[7]});
+    }
 }
 template <typename T> __device__ __forceinline__ int64_t bytes_of(int64_t n) { return n * (16 / T::EPL); }
 
@@ -290,7 +323,7 @@ __global__ __launch_bounds__(256) void moe_dispatch_kernel(const DispatchParams 
 // =============================================================================
 // Combine: the same split; NR rows are in flight at a time.
 // =============================================================================
-template <typename TY, typename TO, int NG>
+template <typename TY, typename TO, int NG, bool NT>
 __global__ __launch_bounds__(256) void moe_combine_kernel(const CombineParams p, int segs) {
     constexpr int NR = 4;
     const int lane = threadIdx.x & 63;
@@ -338,7 +371,7 @@ __global__ __launch_bounds__(256) void moe_combine_kernel(const CombineParams p,
     }
 #pragma unroll
     for (int c = 0; c < NG; ++c)
-        store8<TO>(p.out + token * p.ldo_bytes + bytes_of<TO>(col0 + c * 512), acc[c], p.cols - col0 - c * 512);
+        store8<TO, NT>(p.out + token * p.ldo_bytes + bytes_of<TO>(col0 + c * 512), acc[c], p.cols - col0 - c * 512);
 }
 
 // =============================================================================
@@ -346,7 +379,7 @@ __global__ __launch_bounds__(256) void moe_combine_kernel(const CombineParams p,
 // from memory once.  dy is the weight times that gradient; dw is summed lane by lane over the columns, then over the
 // lanes, always in the same order.
 // =============================================================================
-template <typename TY, typename TO>
+template <typename TY, typename TO, bool NT>
 __global__ __launch_bounds__(256) void moe_combine_bwd_kernel(const CombineParams p) {
     constexpr int NG = 4;
     const int lane = threadIdx.x & 63;
@@ -377,7 +410,7 @@ __global__ __launch_bounds__(256) void moe_combine_bwd_kernel(const CombineParam
                     dot = __builtin_fmaf(dv[e], yv[e], dot);
                     dv[e] *= w;
                 }
-                store8<TY>(dy + bytes_of<TY>(c0 + c * 512), dv, p.cols - c0 - c * 512);
+                store8<TY, NT>(dy + bytes_of<TY>(c0 + c * 512), dv, p.cols - c0 - c * 512);
             }
         }
 #pragma unroll
@@ -459,42 +492,48 @@ ds3_status launch_moe_dispatch(const DispatchParams& p, ds3_dtype xt, DispatchTo
     return launch_status();
 }
 
-template <typename TY, typename TO>
-static void combine_as(const CombineParams& p, int ng, unsigned grid, int segs, hipStream_t st) {
-    if (ng == 1) moe_combine_kernel<TY, TO, 1><<<dim3(grid), 256, 0, st>>>(p, segs);
-    else moe_combine_kernel<TY, TO, 2><<<dim3(grid), 256, 0, st>>>(p, segs);
-}
+// Whether what combine and its gradients write carries the non-temporal hint: where it is so much that little of it would be
+// left in the caches for the next reader.  us without / with it: gradients of 8192 tokens of 7168 columns, one row each on
+// average (117 MB), 68 / 56, eight (940 MB) 405 / 394, of 512 tokens with eight (59 MB) 23.4 / 25.2; the sums of 8192 tokens
+// with eight 192 / 184.
+static bool streams_past(int64_t rows, int64_t row_bytes) { return rows * row_bytes >= (64ll << 20); }
 
-ds3_status launch_moe_combine(const CombineParams& p, ds3_dtype yt, ds3_dtype ot, hipStream_t st) {
+template <typename TY, typename TO, bool NT>
+static void combine_as(const CombineParams& p, int ng, unsigned grid, int segs, hipStream_t st) {
+    if (ng == 1) moe_combine_kernel<TY, TO, 1, NT><<<dim3(grid), 256, 0, st>>>(p, segs);
+    else moe_combine_kernel<TY, TO, 2, NT><<<dim3(grid), 256, 0, st>>>(p, segs);
+}
+template <typename TY, typename TO>
+static ds3_status combine(const CombineParams& p, hipStream_t st) {
     // (8192 tokens of 7168 columns with one row each on average, 1 / 2 units: 47 / 43 us; 64 tokens with eight 4.3 / 5.3)
     const int ng = std::min(2, columns_per_wave(p.tokens, p.cols));
     int segs;
     const unsigned grid = wave_grid(p.tokens, p.cols, ng, &segs);
     if (grid == 0) return DS3_ERR_UNSUPPORTED;
     (void)hipGetLastError();
-    if (yt == DS3_BF16) {
-        if (ot == DS3_BF16) combine_as<Bf16, Bf16>(p, ng, grid, segs, st);
-        else combine_as<Bf16, F32>(p, ng, grid, segs, st);
-    } else {
-        if (ot == DS3_BF16) combine_as<F32, Bf16>(p, ng, grid, segs, st);
-        else combine_as<F32, F32>(p, ng, grid, segs, st);
-    }
+    if (streams_past(p.tokens, p.cols * (16 / TO::EPL))) combine_as<TY, TO, true>(p, ng, grid, segs, st);
+    else combine_as<TY, TO, false>(p, ng, grid, segs, st);
     return launch_status();
 }
-
-ds3_status launch_moe_combine_bwd(const CombineParams& p, ds3_dtype yt, ds3_dtype ot, hipStream_t st) {
+template <typename TY, typename TO>
+static ds3_status combine_bwd(const CombineParams& p, hipStream_t st) {
     const int64_t n = (p.tokens * p.top_k + 3) / 4;
     if (n > kMaxGrid) return DS3_ERR_UNSUPPORTED;
     (void)hipGetLastError();
     const dim3 grid((unsigned)n);
-    if (yt == DS3_BF16) {
-        if (ot == DS3_BF16) moe_combine_bwd_kernel<Bf16, Bf16><<<grid, 256, 0, st>>>(p);
-        else moe_combine_bwd_kernel<Bf16, F32><<<grid, 256, 0, st>>>(p);
-    } else {
-        if (ot == DS3_BF16) moe_combine_bwd_kernel<F32, Bf16><<<grid, 256, 0, st>>>(p);
-        else moe_combine_bwd_kernel<F32, F32><<<grid, 256, 0, st>>>(p);
-    }
+    if (streams_past(std::min(p.total_rows, p.tokens * p.top_k), p.cols * (16 / TY::EPL))) moe_combine_bwd_kernel<TY, TO, true><<<grid, 256, 0, st>>>(p);
+    else moe_combine_bwd_kernel<TY, TO, false><<<grid, 256, 0, st>>>(p);
     return launch_status();
+}
+
+ds3_status launch_moe_combine(const CombineParams& p, ds3_dtype yt, ds3_dtype ot, hipStream_t st) {
+    if (yt == DS3_BF16) return ot == DS3_BF16 ? combine<Bf16, Bf16>(p, st) : combine<Bf16, F32>(p, st);
+    return ot == DS3_BF16 ? combine<F32, Bf16>(p, st) : combine<F32, F32>(p, st);
+}
+
+ds3_status launch_moe_combine_bwd(const CombineParams& p, ds3_dtype yt, ds3_dtype ot, hipStream_t st) {
+    if (yt == DS3_BF16) return ot == DS3_BF16 ? combine_bwd<Bf16, Bf16>(p, st) : combine_bwd<Bf16, F32>(p, st);
+    return ot == DS3_BF16 ? combine_bwd<F32, Bf16>(p, st) : combine_bwd<F32, F32>(p, st);
 }
 
 }  // namespace ds3
