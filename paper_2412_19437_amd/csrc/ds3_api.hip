@@ -565,9 +565,10 @@ ds3_status ds3_dequant_mxfp4(const uint8_t* q, int64_t rows, int64_t cols, int64
     return launch_dequant_mxfp4(q, rows, cols, ldq, s, s_stride_row, s_stride_kb, y, ldy, static_cast<hipStream_t>(stream));
 }
 
-// The kernels address a matrix's scale words with byte offsets below 2^31 and non-negative strides.
+// The kernels address a matrix's scale words with non-negative strides and byte offsets of whole words below the 2^31 - 4
+// bytes that their descriptors span.
 static bool scale_words_fit(int64_t rows, int64_t kw, int64_t sr, int64_t sk) {
-    const int64_t lim = (1ll << 29) - 1;
+    const int64_t lim = (1ll << 29) - 2;
     if (sr < 0 || sk < 0) return false;
     if (rows - 1 > lim / (sr > 0 ? sr : 1) || kw - 1 > lim / (sk > 0 ? sk : 1)) return false;
     return (rows - 1) * sr + (kw - 1) * sk <= lim;

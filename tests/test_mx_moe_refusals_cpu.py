@@ -66,7 +66,7 @@ def test_products(pkg, mem):
         assert _try(fn, good, **bad) == SHAPE, bad
     for bad in (dict(a=mem + 8), dict(b=mem + 8), dict(c=mem + 8), dict(lda=136), dict(ldb=136), dict(ldc=26), dict(sa=mem + 2)):
         assert _try(fn, good, **bad) == ALIGN, bad
-    for bad in (dict(sar=-1), dict(sbk=-1), dict(sak=1 << 29), dict(sbr=1 << 26), dict(lda=1 << 23), dict(ldb=1 << 23), dict(M=1 << 31),
+    for bad in (dict(sar=-1), dict(sbk=-1), dict(sak=1 << 29), dict(sar=0, sak=(1 << 29) - 1), dict(sbr=1 << 26), dict(lda=1 << 23), dict(ldb=1 << 23), dict(M=1 << 31),
                 dict(lda=1 << 31)):
         assert _try(fn, good, **bad) == UNSUPPORTED, bad
     assert _try(fn, good, M=0, a=None, c=None) == 0 and _try(fn, good, N=0) == 0
