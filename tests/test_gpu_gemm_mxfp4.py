@@ -130,6 +130,23 @@ def test_equal_scales_are_exact(ds3, M, N, K):
     assert np.array_equal(y.double().cpu().numpy(), a @ b.T)
 
 
+@pytest.mark.parametrize("M,N,K", [(19, 44, 640), (300, 716, 384), (530, 2300, 896)])
+def test_output_rows_that_begin_on_eight_bytes(ds3, M, N, K):
+    """A leading dimension of four elements more than a multiple of eight: BF16 rows are not 16-byte aligned."""
+    rng = np.random.default_rng(N)
+    a, qa, sa = operand(rng, M, K)
+    b, qb, sb = operand(rng, N, K)
+    want = a @ b.T
+    ld = N // 8 * 8 + 12
+    c = torch.full((M, ld), 1.5, dtype=torch.bfloat16, device=DEV)
+    ds3.ds3_gemm_mxfp4(qa, words(sa), qb, words(sb), c=c[:, :N])
+    assert (np.abs(c[:, :N].double().cpu().numpy() - want) <= allowed(a, b, want, K, True)).all() and (c[:, N:] == 1.5).all()
+    off = torch.tensor([0, M // 3, M], dtype=torch.int32, device=DEV)
+    c.fill_(1.5)
+    ds3.ds3_grouped_gemm_mxfp4(qa, words(sa), off, qb.contiguous().view(1, N, K // 2).repeat(2, 1, 1), words(sb, False)[None].repeat(2, 1, 1), c=c[:, :N])
+    assert (np.abs(c[:, :N].double().cpu().numpy() - want) <= allowed(a, b, want, K, True)).all() and (c[:, N:] == 1.5).all()
+
+
 @pytest.mark.parametrize("M,N,K", [(20, 48, 384), (300, 264, 1152)])
 def test_nan_scales_stay_in_their_rows_and_columns(ds3, M, N, K):
     rng = np.random.default_rng(1)
