@@ -592,7 +592,8 @@ int ds3_gemm_mxfp4_config(int32_t G, int64_t M, int64_t N, int64_t K, int comput
  * padding has) leave no row; a token may choose an expert more than once.
  *   group_offsets [G+1]            row offsets of the experts' groups, as the grouped GEMMs take them
  *   row_of_slot   [tokens][top_k]  row of each choice, ordered by (expert, token, slot), or -1
- * tokens == 0 makes offsets of zero.  top_k <= 64, G <= 1023, tokens * top_k <= 2^31 - 8192.
+ * tokens == 0 makes offsets of zero.  top_k <= 64, G <= 1023, first_expert + G <= 2^31,
+ * tokens * top_k <= 2^31 - 8192.
  *
  * ds3_moe_dispatch: x [tokens][ldx]; y[row_of_slot[t][j]] = x[t] for every choice whose row is
  * in [0, total_rows); other rows of y are left untouched.  y has x's type.  The _quant_ forms

@@ -637,6 +637,7 @@ ds3_status ds3_moe_sort(const int32_t* expert_ids, int64_t tokens, int32_t top_k
     const ds3_status st = check_slots(tokens, 0, top_k, 0);
     if (st != DS3_OK) return st;
     if (G < 0 || first_expert < 0 || ld_ids < top_k) return DS3_ERR_SHAPE;
+    if (first_expert > (1ll << 31) - G) return DS3_ERR_SHAPE;       // (ids are 32-bit: the kernels' differences would wrap)
     if (G > 1023) return DS3_ERR_UNSUPPORTED;
     if (!group_offsets || (tokens > 0 && (!expert_ids || !row_of_slot))) return DS3_ERR_NULL;
     if (!aligned4(expert_ids) || !aligned4(group_offsets) || !aligned4(row_of_slot)) return DS3_ERR_ALIGN;

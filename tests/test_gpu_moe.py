@@ -49,6 +49,22 @@ def test_sort_of_many_choices(ds3, n, k, experts, groups, first):
         assert np.array_equal(off.cpu().numpy(), woff) and np.array_equal(rows.cpu().numpy(), wrows)
 
 
+def test_sort_of_the_last_numbers_and_at_the_longest_single_launch(ds3):
+    """Experts up to 2^31 - 1: the lowest numbers are not theirs.  A packed list, its copy that begins on another border, and
+    one choice more."""
+    first = 2**31 - 7
+    for n in (40, 9000, 131072, 131073):
+        ids = np.random.default_rng(n).choice(np.array([first - 1, first, first + 3, 2**31 - 1, -(2**31), -(2**31) + 2, -1, 0], np.int64), (n, 1)).astype(np.int32)
+        off_border = torch.zeros(n + 1, dtype=torch.int32, device=DEV)[1:].view(n, 1)
+        off_border.copy_(torch.from_numpy(ids))
+        for t in (torch.from_numpy(ids).to(DEV), off_border):
+            off, rows = ds3.ds3_moe_sort(t, 7, first_expert=first)
+            woff, wrows = sort_by_keys(ids, 7, first)
+            assert np.array_equal(off.cpu().numpy(), woff) and np.array_equal(rows.cpu().numpy(), wrows)
+    with pytest.raises(RuntimeError):
+        ds3.ds3_moe_sort(t, 8, first_expert=first)
+
+
 CASES = [(1, 1, 8, 8, 0), (1, 8, 16, 128, 0), (5, 2, 4, 40, 1), (17, 3, 8, 136, 0), (40, 6, 60, 2048, 4), (33, 8, 32, 2056, 0), (9, 64, 7, 264, 0),
          (6, 4, 8, 8200, 0), (70, 5, 64, 1000, 10)]
 

@@ -99,7 +99,7 @@ def test_expert_order(pkg, mem):
     good = dict(ids=mem, tokens=8, k=2, ld=2, first=0, G=4, off=mem, rows=mem, st=None)
     for key in ("ids", "off", "rows"):
         assert _try(L.ds3_moe_sort, good, **{key: None}) == NULL
-    for bad in (dict(tokens=-1), dict(k=0), dict(ld=1), dict(first=-1), dict(G=-1)):
+    for bad in (dict(tokens=-1), dict(k=0), dict(ld=1), dict(first=-1), dict(G=-1), dict(first=(1 << 31) - 3)):
         assert _try(L.ds3_moe_sort, good, **bad) == SHAPE, bad
     assert _try(L.ds3_moe_sort, good, k=65, ld=65) == UNSUPPORTED and _try(L.ds3_moe_sort, good, G=1024) == UNSUPPORTED
     assert _try(L.ds3_moe_sort, good, tokens=1 << 30) == UNSUPPORTED
