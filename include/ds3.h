@@ -605,8 +605,9 @@ int ds3_gemm_mxfp4_config(int32_t G, int64_t M, int64_t N, int64_t K, int comput
  * zeros).  weights [tokens][top_k] FP32, or NULL for ones: the gradient of the dispatch.
  * ds3_moe_combine_bwd: for every choice with a row,
  *   dy[row] = weights[t][j] * dout[t],   dweights[t][j] = sum over c of dout[t][c] * y[row][c]
- * in FP32; dweights is 0 for the others, other rows of dy are left untouched.  dy has y's type.
- * No two choices may name the same row (the sort's never do).
+ * in FP32; dweights is 0 for the others (and all of it without columns), other rows of dy are
+ * left untouched.  dy has y's type.
+ * Where rows are written (dispatch, combine_bwd) no two choices may name the same one (the sort's never do).
  *
  * All matrices 16-byte aligned with rows of whole 16 bytes (cols and ld times the element's
  * size; codes: ldq % 16 == 0).  The types of y and out / dout are independent.

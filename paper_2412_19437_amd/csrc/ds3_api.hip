@@ -719,8 +719,8 @@ ds3_status ds3_moe_combine_bwd(const void* dout, ds3_dtype ot, int64_t ldo, cons
     if (!dtype_ok(yt) || !dtype_ok(ot)) return DS3_ERR_DTYPE;
     ds3_status st = check_slots(tokens, cols, top_k, total_rows);
     if (st != DS3_OK) return st;
-    if (tokens == 0 || cols == 0) return DS3_OK;
-    if (!row_of_slot || !dout || !dweights || (total_rows > 0 && (!y || !dy))) return DS3_ERR_NULL;
+    if (tokens == 0) return DS3_OK;                           // (without columns the weights still have a gradient: zeros)
+    if (!row_of_slot || !dweights || (cols > 0 && (!dout || (total_rows > 0 && (!y || !dy))))) return DS3_ERR_NULL;
     st = check_combine(y, yt, ldy, dout, ot, ldo, cols, row_of_slot, weights);
     if (st != DS3_OK) return st;
     if (lddy < cols) return DS3_ERR_SHAPE;

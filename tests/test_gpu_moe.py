@@ -189,6 +189,19 @@ def test_gradients_against_differences(ds3):
         assert abs(diff - float(dy[hrows[t, j], 7])) <= slack
 
 
+def test_combine_without_columns_or_rows(ds3):
+    """Sums over nothing are zeros, in what the gradients write too."""
+    rng, rows, hrows, total = layout(ds3, 9, 3, 6, 1, 5, spare=0)
+    for cols, held in ((0, total), (64, 0)):
+        y, d = torch.ones((held, cols), device=DEV), torch.ones((9, cols), device=DEV)
+        dw = torch.full((9, 3), 5.0, device=DEV)               # (so that what the call allocates next holds no zeros yet)
+        del dw
+        dy, dw = ds3.ds3_moe_combine_bwd(d, y, rows, torch.rand((9, 3), device=DEV))
+        assert dy.shape == y.shape and torch.equal(dw, torch.zeros((9, 3), device=DEV))
+        out = ds3.ds3_moe_combine(y, rows, torch.rand((9, 3), device=DEV))
+        assert out.shape == (9, cols) and (out == 0).all()
+
+
 def test_combine_without_weights_is_the_gradient_of_dispatch(ds3):
     rng, rows, hrows, total = layout(ds3, 50, 4, 12, 3, 8, spare=0)
     x, g = torch.randn((50, 72), device=DEV), torch.randn((total, 72), device=DEV)

@@ -134,6 +134,7 @@ def test_expert_order(pkg, mem):
     for key in ("d", "y", "rows", "dy", "dw"):
         assert _try(fn, good, **{key: None}) == NULL
     assert _try(fn, good, yt=2) == DTYPE and _try(fn, good, lddy=120) == SHAPE and _try(fn, good, lddy=132) == ALIGN
+    assert _try(fn, good, cols=0, d=None, y=None, dy=None, dw=None) == NULL       # (zeros are written there)
     assert _try(fn, good, dy=mem + 8) == ALIGN and _try(fn, good, dw=mem + 2) == ALIGN and _try(fn, good, tokens=1 << 27) == UNSUPPORTED
 
 
