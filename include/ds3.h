@@ -553,7 +553,7 @@ ds3_status ds3_dequant_mxfp4(const uint8_t* q, int64_t rows, int64_t cols, int64
  *   a [M][lda] codes, b [N][ldb] codes (lda, ldb in bytes), sa, sb scale words as above
  *   c [M][ldc] BF16 (round to nearest even) or FP32 (ct); accumulate != 0: C += result, FP32 only.
  * K % 128 == 0; a, b, c 16-byte aligned, lda, ldb % 16 == 0, ldc % 4 == 0; M and N are
- * arbitrary.  Scale strides are non-negative and reach less than 2^29 - 1 words; 257 * lda and
+ * arbitrary up to 2^31 - 256.  Scale strides are non-negative and reach less than 2^29 - 1 words; 257 * lda and
  * 257 * ldb stay below 2^31 - K / 2.  K == 0 is an empty sum, as in ds3_gemm_fp8_bs.
  * Results are deterministic; no workspace is needed.
  *

@@ -574,6 +574,7 @@ static bool scale_words_fit(int64_t rows, int64_t kw, int64_t sr, int64_t sk) {
     return (rows - 1) * sr + (kw - 1) * sk <= lim;
 }
 
+constexpr int64_t kMaxMxDim = kMaxDim - 255;                  // so that 32 bits hold them rounded up to a tile of 256
 static ds3_status gemm_mx(int32_t G, const int32_t* offs, int64_t M, int64_t N, int64_t K, const uint8_t* a, int64_t lda,
                           const uint32_t* sa, int64_t sar, int64_t sak, const uint8_t* b, int64_t ldb, const uint32_t* sb,
                           int64_t sbr, int64_t sbk, void* c, ds3_dtype ct, int64_t ldc, int accumulate, void* stream) {
@@ -584,7 +585,7 @@ static ds3_status gemm_mx(int32_t G, const int32_t* offs, int64_t M, int64_t N, 
     if (!c) return DS3_ERR_NULL;
     if (ldc < N) return DS3_ERR_SHAPE;
     if (!aligned16(c) || ldc % 4) return DS3_ERR_ALIGN;
-    if (M > kMaxDim || N > kMaxDim || K > kMaxDim || G > 1023) return DS3_ERR_UNSUPPORTED;
+    if (M > kMaxMxDim || N > kMaxMxDim || K > kMaxMxDim || G > 1023) return DS3_ERR_UNSUPPORTED;
     if (K == 0)                                               // an empty sum: C += 0, or C = 0
         return accumulate ? DS3_OK : G > 0 ? DS3_ERR_UNSUPPORTED : launch_zero_fill(c, ct, M, N, ldc, static_cast<hipStream_t>(stream));
     if (!a || !b || !sa || !sb || (G > 0 && !offs)) return DS3_ERR_NULL;
@@ -620,7 +621,7 @@ ds3_status ds3_grouped_gemm_mxfp4(int32_t G, const int32_t* group_offsets, int64
 }
 
 int ds3_gemm_mxfp4_config(int32_t G, int64_t M, int64_t N, int64_t K, int compute_units) {
-    if (G < 0 || G > 1023 || M <= 0 || N <= 0 || K <= 0 || K % 128 || M > kMaxDim || N > kMaxDim || K > kMaxDim || compute_units < 8) return -1;
+    if (G < 0 || G > 1023 || M <= 0 || N <= 0 || K <= 0 || K % 128 || M > kMaxMxDim || N > kMaxMxDim || K > kMaxMxDim || compute_units < 8) return -1;
     return gemm_mxfp4_config(G, (int)M, (int)N, (int)K, compute_units / 8 * 8);
 }
 

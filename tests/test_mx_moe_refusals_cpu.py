@@ -69,6 +69,9 @@ def test_products(pkg, mem):
     for bad in (dict(sar=-1), dict(sbk=-1), dict(sak=1 << 29), dict(sar=0, sak=(1 << 29) - 1), dict(sbr=1 << 26), dict(lda=1 << 23), dict(ldb=1 << 23), dict(M=1 << 31),
                 dict(lda=1 << 31)):
         assert _try(fn, good, **bad) == UNSUPPORTED, bad
+    for big in ((1 << 31) - 1, (1 << 31) - 255):                     # tiles of 256 of them would pass 32 bits
+        assert _try(fn, good, M=big, sar=0) == UNSUPPORTED and _try(fn, good, N=big, ldc=1 << 31, sbr=0) == UNSUPPORTED
+        assert pkg._L().ds3_gemm_mxfp4_config(0, big, 64, 128, 256) == -1 and pkg._L().ds3_gemm_mxfp4_config(8, 64, big, 128, 256) == -1
     assert _try(fn, good, M=0, a=None, c=None) == 0 and _try(fn, good, N=0) == 0
     assert _try(fn, good, K=0, ct=0, acc=1, a=None) == 0             # C += an empty sum
     fn = pkg._L().ds3_grouped_gemm_mxfp4
