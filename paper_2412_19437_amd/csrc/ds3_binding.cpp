@@ -458,7 +458,7 @@ PyObject* moe_sort(PyObject*, PyObject* const* o, Py_ssize_t n) {
     const int64_t g = integer(o[1]), first = integer(o[2]);
     need_type(ids, at::kInt, "expert_ids must be int32");
     const Mat m = mat2d(ids, "expert_ids");
-    if (g < 0 || g > INT32_MAX || first < 0 || first > INT32_MAX || m.cols > INT32_MAX) fail(PyExc_ValueError, "bad number of experts");
+    if (g < 0 || g > 1023 || first < 0 || first > INT32_MAX || m.cols > INT32_MAX) fail(PyExc_ValueError, "num_experts is 0 .. 1023, first_expert 0 .. 2^31 - 1");
     const auto opt = at::TensorOptions().dtype(at::kInt).device(ids.device());
     const at::Tensor off = at::empty({g + 1}, opt), rows = at::empty({m.rows, m.cols}, opt);
     void* st = stream();
