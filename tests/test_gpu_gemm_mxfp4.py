@@ -173,6 +173,67 @@ def test_empty_sums_and_extreme_scales(ds3):
     assert (y == 256.0).all()
 
 
+@pytest.mark.parametrize("M,N", [(3, 40), (40, 700), (300, 400), (1100, 2100)])
+@pytest.mark.parametrize("K", [128, 384, 1024, 1664])
+def test_zeros_under_the_largest_scales(ds3, M, N, K):
+    """0 * 2^127 * 2^127 is 0, in a half K-step's empty half too; a one among them is 2^254, an infinity."""
+    qa, qb = torch.zeros((M, K // 2), dtype=torch.uint8, device=DEV), torch.full((N, K // 2), 0x22, dtype=torch.uint8, device=DEV)
+    sa, sb = (torch.full((n, K // 128), -0x01010102, dtype=torch.int32, device=DEV) for n in (M, N))
+    assert (ds3.ds3_gemm_mxfp4(qa, sa, qb, sb, out_dtype=torch.float32) == 0).all()
+    qa[M // 2, K // 2 - 1] = 0x20
+    y = ds3.ds3_gemm_mxfp4(qa, sa, qb, sb, out_dtype=torch.float32)
+    assert (y[M // 2] == float("inf")).all() and (y == 0).sum() == (M - 1) * N
+
+
+@pytest.mark.parametrize("sizes", [(2, 0, 9), (30, 50, 41), (150, 100, 0, 130), (256, 700)])
+def test_groups_that_begin_behind_the_first_row(ds3, sizes):
+    rng = np.random.default_rng(sum(sizes))
+    G, N, K, rows = len(sizes), 1032, 640, sum(sizes) + 20
+    off = (7 + np.concatenate([[0], np.cumsum(sizes)])).astype(np.int32)
+    a, qa, sa = operand(rng, rows, K)
+    b, qb, sb = operand(rng, G * N, K)
+    c = torch.full((rows, N), 5.0, device=DEV)
+    y = ds3.ds3_grouped_gemm_mxfp4(qa, words(sa), torch.from_numpy(off).to(DEV), qb.contiguous().view(G, N, K // 2), words(sb, False).view(G, N, K // 128),
+                                   c=c).double().cpu().numpy()
+    assert (y[:7] == 5).all() and (y[off[-1]:] == 5).all()
+    for g in range(G):
+        at, bg = slice(off[g], off[g + 1]), b[g * N : (g + 1) * N]
+        want = a[at] @ bg.T
+        assert (np.abs(y[at] - want) <= allowed(a[at], bg, want, K, False)).all()
+
+
+@pytest.mark.parametrize("M,N,K", [(5, 96, 512), (200, 640, 384), (1200, 2304, 640)])
+def test_captured(ds3, M, N, K):
+    """Quantizers, products (one adding to what is there) and the way back in a graph, replayed on other values between eager work."""
+    gen = torch.Generator(device=DEV).manual_seed(N)
+    make = lambda *s: torch.randn(s, generator=gen, device=DEV)
+    x, w, c = make(M, K).bfloat16(), make(K, N), make(M, N)
+
+    def step(c):
+        q, s = ds3.ds3_quant_mxfp4(x)
+        qw, sw = ds3.ds3_quant_mxfp4_t(w)
+        return ds3.ds3_gemm_mxfp4(q, s, qw, sw), ds3.ds3_gemm_mxfp4(q, s, qw, sw, c=c, accumulate=True), ds3.ds3_dequant_mxfp4(q, s), qw, sw
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(c.clone())
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        outs = step(c)
+    for i in range(4):
+        x.copy_(make(M, K))
+        w.copy_(make(K, N) * 2.0 ** i)
+        c.copy_(make(M, N))
+        want = step(c.clone())
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(o, v) for o, v in zip(outs, want))
+        make(64, 64).sum().item()
+
+
 @pytest.mark.parametrize("sizes,N,K", [((0, 5, 0, 1, 40, 0), 200, 384), ((130, 0, 257, 3), 264, 512), ((1,) * 70 + (0,) * 3 + (20,), 64, 256),
                                        ((0, 0, 0), 32, 128), ((33, 90, 64, 300, 12), 1024, 1152), ((700, 1, 500), 384, 256)])
 def test_grouped(ds3, sizes, N, K):
