@@ -325,6 +325,9 @@ struct MxTile {
 template <class C, bool OUT_BF16, bool GROUPED>
 __global__ __launch_bounds__(C::NT) void gemm_mxfp4_kernel(const MxGemmParams p) {
     constexpr int BN = C::BN, BM = C::BM, NT = C::NT, NS = C::NS, FN = C::FN, FM = C::FM, STAGE = C::STAGE;
+    // The way out: PASSES times 64 lanes x 16 bytes are 16 rows x TN columns, through an LDS strip a wave in the last stage.
+    constexpr int ESZ = OUT_BF16 ? 2 : 4, SEG = C::TN * ESZ, ROWB = SEG + 16, CPR = SEG / 16, PASSES = 16 * CPR / 64, STORES = FM * PASSES;
+    static_assert(16 * CPR % 64 == 0, "epilogue mapping");
     __shared__ __attribute__((aligned(1024))) uint8_t smem[C::LDS_BYTES];
     uint8_t* const scales = smem + NS * STAGE;
     int* const before = reinterpret_cast<int*>(scales + NS * C::SSTAGE);       // [G + 1] row tiles before expert g
@@ -468,9 +471,9 @@ __global__ __launch_bounds__(C::NT) void gemm_mxfp4_kernel(const MxGemmParams p)
     // Barrier that lets the newest `keep` vector-memory operations of this wave stay in flight.
     auto barrier_keep = [&](auto keep_tag) {
         constexpr int keep = decltype(keep_tag)::value;
-        static_assert(keep >= 0 && keep < 16, "vmcnt immediate");
+        static_assert(keep >= 0 && keep < 64, "vmcnt immediate");
         asm volatile("" ::: "memory");
-        __builtin_amdgcn_s_waitcnt(keep | 0x70);       // vmcnt(keep) lgkmcnt(0)
+        __builtin_amdgcn_s_waitcnt((keep & 15) | ((keep >> 4) << 14) | 0x70);      // vmcnt(keep) lgkmcnt(0)
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
@@ -489,14 +492,30 @@ __global__ __launch_bounds__(C::NT) void gemm_mxfp4_kernel(const MxGemmParams p)
         }
     };
 
+    // Barrier that lets the newest `steps` K-steps' loads stay in flight, and the previous tile's stores with them: those are
+    // waited for only where data asked for behind them is needed (vector-memory operations end in order).  us without / with
+    // it: 4096x18432x7168 256 / 251, FP32 4096x16384x7168 254 / 243, added to what was there 308 / 314, 7168x7168x4096 added
+    // 174 / 166.  Strips outside the stages, so that two K-steps run before the stores have to be done, need an own form of
+    // the first K-step, whose registers spill: 264.
+    bool flying = false;                               // whether this wave has issued STORES stores behind the first loads
+    auto barrier_flying = [&](auto steps_tag) {
+        constexpr int steps = decltype(steps_tag)::value, few = steps * C::LPT, many = steps * (C::LPT + 2);
+        if (scale_role) {
+            if (flying) barrier_keep(std::integral_constant<int, many + STORES>{});
+            else barrier_keep(std::integral_constant<int, many>{});
+        } else {
+            if (flying) barrier_keep(std::integral_constant<int, few + STORES>{});
+            else barrier_keep(std::integral_constant<int, few>{});
+        }
+    };
+
     MxTile cur;
     int unit = 0;
     if (!setup(unit, cur)) return;
     issue_first_steps(cur);
     for (;;) {
-        // ---- K-steps 0 .. NS-2 of `cur` are in flight into stages 0 .. NS-2 ----
-        __builtin_amdgcn_s_waitcnt(0x70);
-        __syncthreads();
+        // ---- K-steps 0 .. NS-2 of `cur` are in flight into stages 0 .. NS-2, and behind them the stores ----
+        barrier_flying(std::integral_constant<int, NS - 2>{});
         {
             const unsigned koff = koff_of(NS - 1);
 #pragma unroll
@@ -518,7 +537,8 @@ __global__ __launch_bounds__(C::NT) void gemm_mxfp4_kernel(const MxGemmParams p)
 #pragma unroll
             for (int j = 0; j < FM; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-        auto kstep = [&](int kb, auto stage_tag) {
+        auto kstep = [&](int kb, auto stage_tag, auto first_tag) {
+            constexpr bool FIRST = decltype(first_tag)::value;         // the stores may be in flight behind what its barrier waits for
             constexpr int S = decltype(stage_tag)::value, SN = (S + 1) % NS, SL = (S + NS - 1) % NS;
             const uint8_t* st = smem + S * STAGE;
             const uint8_t* nst = smem + SN * STAGE;
@@ -530,7 +550,8 @@ __global__ __launch_bounds__(C::NT) void gemm_mxfp4_kernel(const MxGemmParams p)
 #pragma unroll
             for (int j = 0; j < FM; ++j) {
                 if (j == FM - 1) {
-                    kstep_barrier();
+                    if constexpr (FIRST) barrier_flying(std::integral_constant<int, NS - 2>{});
+                    else kstep_barrier();
                     __builtin_amdgcn_sched_barrier(0);
                 }
 #pragma unroll
@@ -563,12 +584,14 @@ __global__ __launch_bounds__(C::NT) void gemm_mxfp4_kernel(const MxGemmParams p)
             }
         };
         // The same for a wave whose rows all lie beyond the tile's: it moves its share of the data, in the same order.
-        auto kstep_idle = [&](int kb, auto stage_tag) {
+        auto kstep_idle = [&](int kb, auto stage_tag, auto first_tag) {
+            constexpr bool FIRST = decltype(first_tag)::value;
             constexpr int S = decltype(stage_tag)::value, SL = (S + NS - 1) % NS;
             const unsigned koff1 = koff_of(kb + NS - 1), koff2 = koff_of(kb + NS);
 #pragma unroll
             for (int i = 0; i < C::HEADN; ++i) issue_load(cur, C::TAILN + i, SL, koff1);
-            kstep_barrier();
+            if constexpr (FIRST) barrier_flying(std::integral_constant<int, NS - 2>{});
+            else kstep_barrier();
             issue_load(cur, 0, S, koff2);
             issue_scales(cur, kb + NS, S);
 #pragma unroll
@@ -579,21 +602,23 @@ __global__ __launch_bounds__(C::NT) void gemm_mxfp4_kernel(const MxGemmParams p)
         using st2 = std::integral_constant<int, 2>;
         const bool active = wm * C::TM < cur.m_rows;    // wave-uniform
         auto kloop = [&](auto step) {
+            std::false_type other;
             int kb = 0;
             if constexpr (NS == 2) {
                 for (; kb + 1 < KB; kb += 2) {
-                    step(kb, st0{});
-                    step(kb + 1, st1{});
+                    step(kb, st0{}, other);
+                    step(kb + 1, st1{}, other);
                 }
-                if (kb < KB) step(kb, st0{});
+                if (kb < KB) step(kb, st0{}, other);
             } else {
+                step(kb++, st0{}, std::true_type{});
                 for (; kb + 2 < KB; kb += 3) {
-                    step(kb, st0{});
-                    step(kb + 1, st1{});
-                    step(kb + 2, st2{});
+                    step(kb, st1{}, other);
+                    step(kb + 1, st2{}, other);
+                    step(kb + 2, st0{}, other);
                 }
-                if (kb < KB) step(kb, st0{});
-                if (kb + 1 < KB) step(kb + 1, st1{});
+                if (kb < KB) step(kb, st1{}, other);
+                if (kb + 1 < KB) step(kb + 1, st2{}, other);
             }
         };
         if (active) kloop(kstep);
@@ -601,41 +626,40 @@ __global__ __launch_bounds__(C::NT) void gemm_mxfp4_kernel(const MxGemmParams p)
         __builtin_amdgcn_s_waitcnt(0x70);              // nothing is on its way into the stages any more
         __syncthreads();                               // every wave is done with all of them
 
-        // ---- the next tile's first K-steps fly into stages 0 .. NS-2 during this one's way out ----
+        // ---- the next tile's first K-steps fly into their stages during this one's way out ----
         MxTile nxt;
         ++unit;
         const bool more = setup(unit, nxt);
         if (more) issue_first_steps(nxt);
+        asm volatile("" ::: "memory");                 // (the stores are counted on to be behind these loads)
+        __builtin_amdgcn_sched_barrier(0);
         // A lane owns one activation row and, per weight fragment, four consecutive columns: each wave turns 16 rows x
-        // TN columns at a time through an LDS strip of its own in the last stage, so that stores are 16 bytes a lane
-        // and whole 128- or 256-byte row segments (64-byte ones straight from the registers: 257 -> 271 us with
-        // non-temporal stores, 264 with plain ones).
+        // TN columns at a time through its LDS strip, so that stores are 16 bytes a lane and whole 128- or 256-byte row
+        // segments (64-byte ones straight from the registers: 257 -> 271 us with non-temporal stores, 264 with plain ones).
         // (every address here derives from this copy of the thread index, which the compiler cannot see through: none is
         // computed before the K-loop and kept in a register across it)
         int tid_e = threadIdx.x;
         asm volatile("" : "+v"(tid_e));
         const int lane = tid_e & 63, l16 = tid_e & 15, g4 = (tid_e >> 4) & 3;
-        constexpr int ESZ = OUT_BF16 ? 2 : 4;
-        constexpr int SEG = C::TN * ESZ, ROWB = SEG + 16, CPR = SEG / 16, PASSES = 16 * CPR / 64;
-        static_assert(16 * CPR % 64 == 0, "epilogue mapping");
         uint8_t* strip = smem + (NS - 1) * STAGE + wave * (16 * ROWB);
         uint64_t c_bits = reinterpret_cast<uint64_t>(p.c);
         int64_t ldc = p.ldc;
         asm volatile("" : "+s"(c_bits), "+s"(ldc));    // (registers of their own: not re-read in front of every store)
         uint8_t* c_base = (uint8_t*)(__attribute__((address_space(1))) uint8_t*)c_bits;
-        if (active) {
+        // FULL: all of the wave's rows and columns are the tile's, so it issues exactly STORES stores.  (ADD, what was there
+        // is added to, is settled outside: behind a branch inside, every store would wait for loads.)
+        auto way_out = [&](auto full_tag, auto add_tag) {
+            constexpr bool FULL = decltype(full_tag)::value, ADD = decltype(add_tag)::value;
 #pragma unroll
             for (int j = 0; j < FM; ++j) {
                 [[maybe_unused]] f32x4 old[PASSES];    // (16 rows further ahead they would not fit beside the sums: 332 -> 355 us)
-                if constexpr (!OUT_BF16) {
-                    if (p.accumulate) {
+                if constexpr (ADD) {
 #pragma unroll
-                        for (int ps_ = 0; ps_ < PASSES; ++ps_) {
-                            const int idx = ps_ * 64 + lane, ml = wm * C::TM + j * 16 + idx / CPR, nl = wn * C::TN + (idx % CPR) * 4;
-                            old[ps_] = f32x4{0.f, 0.f, 0.f, 0.f};
-                            if (ml < cur.m_rows && nl + 4 <= cur.n_rows)
-                                old[ps_] = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(c_base + ((int64_t)(cur.m0 + ml) * ldc + cur.n0 + nl) * 4));
-                        }
+                    for (int ps_ = 0; ps_ < PASSES; ++ps_) {
+                        const int idx = ps_ * 64 + lane, ml = wm * C::TM + j * 16 + idx / CPR, nl = wn * C::TN + (idx % CPR) * 4;
+                        old[ps_] = f32x4{0.f, 0.f, 0.f, 0.f};
+                        if (FULL || (ml < cur.m_rows && nl + 4 <= cur.n_rows))
+                            old[ps_] = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(c_base + ((int64_t)(cur.m0 + ml) * ldc + cur.n0 + nl) * 4));
                     }
                 }
 #pragma unroll
@@ -656,15 +680,15 @@ __global__ __launch_bounds__(C::NT) void gemm_mxfp4_kernel(const MxGemmParams p)
                 for (int ps_ = 0; ps_ < PASSES; ++ps_) {
                     const int idx = ps_ * 64 + lane;
                     const int ml = wm * C::TM + j * 16 + idx / CPR, nl = wn * C::TN + (idx % CPR) * (16 / ESZ);
-                    if (ml >= cur.m_rows || nl >= cur.n_rows) continue;
+                    if (!FULL && (ml >= cur.m_rows || nl >= cur.n_rows)) continue;
                     uint8_t* gp = c_base + ((int64_t)(cur.m0 + ml) * ldc + cur.n0 + nl) * ESZ;
                     const u32x4 w = wv[ps_];
-                    if (nl + 16 / ESZ <= cur.n_rows) {
+                    if (FULL || nl + 16 / ESZ <= cur.n_rows) {
                         if constexpr (OUT_BF16) {
                             __builtin_nontemporal_store(w, reinterpret_cast<u32x4*>(gp));
                         } else {
                             f32x4 o = f32x4{as_f32(w.x), as_f32(w.y), as_f32(w.z), as_f32(w.w)};
-                            if (p.accumulate) { const f32x4 v = old[ps_]; o.x += v.x; o.y += v.y; o.z += v.z; o.w += v.w; }
+                            if constexpr (ADD) { const f32x4 v = old[ps_]; o.x += v.x; o.y += v.y; o.z += v.z; o.w += v.w; }
                             __builtin_nontemporal_store(o, reinterpret_cast<f32x4*>(gp));
                         }
                     } else {
@@ -674,13 +698,27 @@ __global__ __launch_bounds__(C::NT) void gemm_mxfp4_kernel(const MxGemmParams p)
                                 reinterpret_cast<uint16_t*>(gp)[q] = (uint16_t)(wd[q >> 1] >> (16 * (q & 1)));
                             } else {
                                 float* d = reinterpret_cast<float*>(gp) + q;
-                                *d = p.accumulate ? *d + as_f32(wd[q]) : as_f32(wd[q]);
+                                *d = ADD ? *d + as_f32(wd[q]) : as_f32(wd[q]);
                             }
                         }
                     }
                 }
                 __builtin_amdgcn_wave_barrier();       // the strip is read before the next rows replace it
+                __builtin_amdgcn_sched_barrier(0);
             }
+        };
+        flying = (wm + 1) * C::TM <= cur.m_rows && (wn + 1) * C::TN <= cur.n_rows;
+        auto leave = [&](auto full_tag) {
+            if constexpr (!OUT_BF16 && !GROUPED) {
+                if (p.accumulate) return way_out(full_tag, std::true_type{});
+            }
+            way_out(full_tag, std::false_type{});
+        };
+        if (flying) {
+            leave(std::true_type{});
+        } else {
+            if (active) leave(std::false_type{});
+            __builtin_amdgcn_s_waitcnt(0xf70);         // (unknown how many: none flies on.  vmcnt(0))
         }
         if (!more) break;
         cur = nxt;
