@@ -200,6 +200,20 @@ __global__ __launch_bounds__(C::NT) void gemm_mxfp4_tile_kernel(const MxGemmPara
     const int so_b = C::GROUP + ((g4 >> 1) * BN + wn * FN * 16 + l16) * 4 + (g4 & 1) * 2;
     const int so_a = C::GROUP + C::LW * 256 + ((g4 >> 1) * BM + l16) * 4 + (g4 & 1) * 2;
 
+    // what a thread writes: four columns of a row, OUTS times; what is there already is on its way during the K-loop
+    // (1536x1000x2048 added to FP32: 9.8 us, read behind it 10.7)
+    constexpr int OUTS = (BM * (BN / 4) + C::NT - 1) / C::NT;
+    constexpr bool MAY_ADD = !OUT_BF16 && !GROUPED;
+    [[maybe_unused]] f32x4 old[OUTS];
+    if constexpr (MAY_ADD) {
+#pragma unroll
+        for (int o = 0; o < OUTS; ++o) {
+            const int idx = tid + o * C::NT, row = idx / (BN / 4), col = idx % (BN / 4) * 4;
+            old[o] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (p.accumulate && row < m_rows && col + 4 <= n_rows)
+                old[o] = *reinterpret_cast<const f32x4*>(static_cast<const float*>(p.c) + (int64_t)(m0 + row) * p.ldc + n0 + col);
+        }
+    }
     const int steps = (KB + WK - 1) / WK;
 #pragma unroll
     for (int s = 0; s < NS - 1; ++s) issue(s, s);
@@ -262,9 +276,10 @@ __global__ __launch_bounds__(C::NT) void gemm_mxfp4_tile_kernel(const MxGemmPara
         for (int i = 0; i < FN; ++i)
             *reinterpret_cast<f32x4*>(red + (wk * BM + j * 16 + l16) * C::RLD + (wn * FN + i) * 16 + g4 * 4) = acc[i][j];
     __syncthreads();
-    for (int idx = tid; idx < m_rows * (BN / 4); idx += C::NT) {
-        const int row = idx / (BN / 4), col = idx % (BN / 4) * 4;
-        if (col >= n_rows) continue;
+#pragma unroll
+    for (int out = 0; out < OUTS; ++out) {
+        const int idx = tid + out * C::NT, row = idx / (BN / 4), col = idx % (BN / 4) * 4;
+        if (row >= m_rows || col >= n_rows) continue;
         f32x4 v = *reinterpret_cast<const f32x4*>(red + row * C::RLD + col);
 #pragma unroll
         for (int g = 1; g < WK; ++g) {
@@ -280,10 +295,7 @@ __global__ __launch_bounds__(C::NT) void gemm_mxfp4_tile_kernel(const MxGemmPara
         } else {
             float* d = static_cast<float*>(p.c) + at;
             if (col + 4 <= n_rows) {
-                if (p.accumulate) {
-                    const f32x4 old = *reinterpret_cast<const f32x4*>(d);
-                    v.x += old.x; v.y += old.y; v.z += old.z; v.w += old.w;
-                }
+                if (MAY_ADD && p.accumulate) { v.x += old[out].x; v.y += old[out].y; v.z += old[out].z; v.w += old[out].w; }
                 *reinterpret_cast<f32x4*>(d) = v;
             } else {
                 const float o[4] = {v.x, v.y, v.z, v.w};
