@@ -668,18 +668,27 @@ __global__ __launch_bounds__(C::NT) void gemm_mxfp4_kernel(const MxGemmParams p)
         // is added to, is settled outside: behind a branch inside, every store would wait for loads.)
         auto way_out = [&](auto full_tag, auto add_tag) {
             constexpr bool FULL = decltype(full_tag)::value, ADD = decltype(add_tag)::value;
+            // of how many 16 rows the old values are fetched at once: of all (2048x2048x4096 22.0 -> 20.1 us), or, beside the sums of a
+            // 128x64 wave tile, of one (of two the registers spill: 332 -> 355)
+            constexpr int OLD = C::NSUB <= 16 ? FM : 1;
+            [[maybe_unused]] f32x4 old[OLD][PASSES];
+            [[maybe_unused]] auto fetch_old = [&](int j, f32x4* into) {
+#pragma unroll
+                for (int ps_ = 0; ps_ < PASSES; ++ps_) {
+                    const int idx = ps_ * 64 + lane, ml = wm * C::TM + j * 16 + idx / CPR, nl = wn * C::TN + (idx % CPR) * 4;
+                    into[ps_] = f32x4{0.f, 0.f, 0.f, 0.f};
+                    if (FULL || (ml < cur.m_rows && nl + 4 <= cur.n_rows))
+                        into[ps_] = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(c_base + ((int64_t)(cur.m0 + ml) * ldc + cur.n0 + nl) * 4));
+                }
+            };
+            if constexpr (ADD && OLD > 1) {
+#pragma unroll
+                for (int j = 0; j < FM; ++j) fetch_old(j, old[j]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
 #pragma unroll
             for (int j = 0; j < FM; ++j) {
-                [[maybe_unused]] f32x4 old[PASSES];    // (16 rows further ahead they would not fit beside the sums: 332 -> 355 us)
-                if constexpr (ADD) {
-#pragma unroll
-                    for (int ps_ = 0; ps_ < PASSES; ++ps_) {
-                        const int idx = ps_ * 64 + lane, ml = wm * C::TM + j * 16 + idx / CPR, nl = wn * C::TN + (idx % CPR) * 4;
-                        old[ps_] = f32x4{0.f, 0.f, 0.f, 0.f};
-                        if (FULL || (ml < cur.m_rows && nl + 4 <= cur.n_rows))
-                            old[ps_] = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(c_base + ((int64_t)(cur.m0 + ml) * ldc + cur.n0 + nl) * 4));
-                    }
-                }
+                if constexpr (ADD && OLD == 1) fetch_old(j, old[0]);
 #pragma unroll
                 for (int i = 0; i < FN; ++i) {
                     const f32x4 v = acc[i][j];
@@ -706,7 +715,7 @@ __global__ __launch_bounds__(C::NT) void gemm_mxfp4_kernel(const MxGemmParams p)
                             __builtin_nontemporal_store(w, reinterpret_cast<u32x4*>(gp));
                         } else {
                             f32x4 o = f32x4{as_f32(w.x), as_f32(w.y), as_f32(w.z), as_f32(w.w)};
-                            if constexpr (ADD) { const f32x4 v = old[ps_]; o.x += v.x; o.y += v.y; o.z += v.z; o.w += v.w; }
+                            if constexpr (ADD) { const f32x4 v = old[j % OLD][ps_]; o.x += v.x; o.y += v.y; o.z += v.z; o.w += v.w; }
                             __builtin_nontemporal_store(o, reinterpret_cast<f32x4*>(gp));
                         }
                     } else {
