@@ -756,11 +756,14 @@ __global__ __launch_bounds__(C::NT) void gemm_mxfp4_kernel(const MxGemmParams p)
 }
 
 // ---- host side -------------------------------------------------------------------
+// Row tiles of a grouped call, an upper bound (a row tile has a row).
+static int64_t most_row_tiles(int G, int M, int bm) { return std::min<int64_t>(((int64_t)M + bm - 1) / bm + G, M); }
+
 template <class C, bool GROUPED>
 static ds3_status launch_tile(MxGemmParams p, ds3_dtype ct, hipStream_t st) {
     p.tiles_m = (p.M + C::BM - 1) / C::BM;
-    // grouped: an upper bound (a row tile has a row); workgroups beyond the true count leave at once
-    if (GROUPED) p.tiles_m = (int)std::min<int64_t>((int64_t)p.tiles_m + p.G, p.M);
+    // (workgroups beyond the true count leave at once)
+    if (GROUPED) p.tiles_m = (int)most_row_tiles(p.G, p.M, C::BM);
     p.tiles_n = (p.N + C::BN - 1) / C::BN;
     const int64_t n = ((int64_t)p.tiles_m * p.tiles_n + 7) / 8 * 8;
     if (n * C::NT >= (1ll << 32)) return DS3_ERR_UNSUPPORTED;
@@ -781,7 +784,7 @@ static int compute_units_x8() {
 template <class C, bool GROUPED>
 static ds3_status launch_main(MxGemmParams p, ds3_dtype ct, int cus, hipStream_t st) {
     p.tiles_m = (p.M + C::BM - 1) / C::BM;
-    if (GROUPED) p.tiles_m = (int)std::min<int64_t>((int64_t)p.tiles_m + p.G, p.M);     // (an upper bound)
+    if (GROUPED) p.tiles_m = (int)most_row_tiles(p.G, p.M, C::BM);
     p.tiles_n = (p.N + C::BN - 1) / C::BN;
     const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n, want = (tiles + 7) / 8 * 8, slots = (int64_t)cus * C::WG_PER_CU;
     if (tiles > (1ll << 31) - 16) return DS3_ERR_UNSUPPORTED;
@@ -835,8 +838,11 @@ static int mx_dense_choice(int M, int N, int K, int cus) {
 enum { kMxG64x32, kMxG128x64, kMxG64x64, kMxG128x128, kMxG256x128, kMxG256x256 };
 static int mx_grouped_choice(int G, int M, int N, int K, int cus) {
     const int64_t mean = ((int64_t)M + G - 1) / G;
-    if (mean <= 24) return kMxG64x32;
-    if (mean <= 48) return kMxG128x64;
+    // (few rows take a workgroup of 256 threads a tile; so many columns that a grid does not hold those go on to larger
+    // tiles, in the end to the workgroups that walk)
+    auto fits = [&](int bn, int bm) { return most_row_tiles(G, M, bm) * (((int64_t)N + bn - 1) / bn) <= (1 << 24) - 8; };
+    if (mean <= 24 && fits(64, 32)) return kMxG64x32;
+    if (mean <= 48 && fits(128, 64)) return kMxG128x64;
     const int most = mean > 96 && mean <= 256 ? kMxG256x256 : kMxG256x128;
     auto tiles_m = [&](int bm) { return (int64_t)M / bm + (G + 1) / 2; };      // (half a tile an expert is lost on average)
     if (tiles_m(most == kMxG256x256 ? 256 : 128) * ((N + 255) / 256) * 4 >= 3 * (int64_t)cus) return most;
