@@ -530,9 +530,11 @@ ds3_status ds3_adamw_bf16_states(int64_t n, float* master_w, const float* grad, 
  *                    that contracts over the rows: a weight for the input's gradient,
  *                    tokens for the weight's).  q_t [cols][ldq], code of (row t, column c)
  *                    in byte c * ldq + t / 2; s_t word of (column c, block of 128 rows rb) at
- *                    s_t[c * s_stride_col + rb * s_stride_rb].  `rows` is arbitrary; an odd
- *                    number of them leaves a code of zero in the last byte's high half.
+ *                    s_t[c * s_stride_col + rb * s_stride_rb].  An odd number of
+ *                    rows leaves a code of zero in the last byte's high half.
  * ds3_dequant_mxfp4: y [rows][ldy] BF16 = decode(q) * s, exact (beyond BF16's range: an infinity).
+ * Sizes that are taken (larger ones: DS3_ERR_UNSUPPORTED): along a row and back ceil(rows / 16) *
+ * ceil(cols / 256) < 2^24; transposed rows <= 65535 * 256 = 16776960, cols <= 2^30 - 64.
  * Alignment: x, y, q 16-byte aligned, ldq % 16 == 0, ldx * sizeof(element), cols *
  * sizeof(element) (not for the dequantizer: any `cols`) and ldy * 2 multiples of 16 bytes.
  */
@@ -559,7 +561,9 @@ ds3_status ds3_dequant_mxfp4(const uint8_t* q, int64_t rows, int64_t cols, int64
  *
  * Grouped over experts as ds3_grouped_gemm_fp8_bs: rows [group_offsets[g], group_offsets[g+1])
  * of a with b[g]; b [G][N][ldb], scale words of expert g from sb + g * N * (K / 128) on, with
- * the strides within.  Rows at or beyond group_offsets[G] are left untouched.  G <= 1023, K > 0.
+ * the strides within.  Rows at or beyond group_offsets[G] are left untouched.  G <= 1023, K > 0,
+ * N * ldb * G <= 2^40.  Which tiles a call takes goes by total_rows / G, since the offsets are on
+ * the device: room for many more rows than the groups have costs time.
  */
 ds3_status ds3_gemm_mxfp4(int64_t M, int64_t N, int64_t K,
                           const uint8_t* a, int64_t lda,
@@ -608,6 +612,9 @@ int ds3_gemm_mxfp4_config(int32_t G, int64_t M, int64_t N, int64_t K, int comput
  * in FP32; dweights is 0 for the others (and all of it without columns), other rows of dy are
  * left untouched.  dy has y's type.
  * Where rows are written (dispatch, combine_bwd) no two choices may name the same one (the sort's never do).
+ * No array that a call writes may overlap one that it reads.
+ * Sizes that are taken (larger ones: DS3_ERR_UNSUPPORTED): dispatch and combine tokens *
+ * ceil(cols / 512) <= 2^26 - 4, combine_bwd tokens * top_k <= 2^26 - 4; the sort takes more choices (above).
  *
  * All matrices 16-byte aligned with rows of whole 16 bytes (cols and ld times the element's
  * size; codes: ldq % 16 == 0).  The types of y and out / dout are independent.
