@@ -471,7 +471,8 @@ def ds3_moe_sort(expert_ids: torch.Tensor, num_experts: int, first_expert: int =
 
 def ds3_moe_dispatch(x: torch.Tensor, row_of_slot: torch.Tensor, rows: int | None = None, out: torch.Tensor | None = None):
     """x [T][H] -> y [rows][H] with y[row_of_slot[t][j]] = x[t]; rows: by default one for every choice.  Choices whose row is
-    not below `rows` are dropped, rows that no choice names are left as they were."""
+    not below `rows` are dropped, rows that no choice names are left as they were.  (With part of the experts here, give about
+    as many rows as are expected: the grouped products choose their tiles by the room.)"""
     return (_native or _load_native()).moe_dispatch(x, row_of_slot, rows, out)
 
 

@@ -27,7 +27,8 @@ __device__ __forceinline__ f32x4 mfma_mx4(const i32x4& a, const i32x4& b, const 
 
 // A workgroup takes BN = 16 FN WN weight rows by BM = 16 FM activation rows, NS stages of LDS, NS - 1 of them in
 // flight; WK groups of WN waves take every WK-th K-step each and their sums meet in LDS in a fixed order.  Bound by the
-// weights' stream where rows are few (16x18432x7168 12.8 us, 5.5 TB/s of weights), by latencies where all is small.
+// weights' stream where rows are few (16x18432x7168 12.7 us, 5.6 TB/s of weights from the memory-side cache; from HBM 14.8 us, 4.8
+// TB/s), by latencies where all is small.
 template <int FN_, int FM_, int WN_, int WK_, int NS_>
 struct TileCfg {
     static constexpr int FN = FN_, FM = FM_, WN = WN_, WK = WK_, NS = NS_;
@@ -307,9 +308,11 @@ __global__ __launch_bounds__(C::NT) void gemm_mxfp4_tile_kernel(const MxGemmPara
 }
 
 // ---- the kernel for many tiles ------------------------------------------------------
-// BN x BM output tiles, WN x WM waves, NS stages of LDS with loads NS - 1 K-steps ahead of the matrix instructions.  Bound by
-// the chip's power: 4096x18432x7168 251 us, 4.3 PFLOP/s, the matrix units busy for 57% of 1.84 GHz (94% of 1.88 GHz in a loop
-// on registers).
+// BN x BM output tiles, WN x WM waves, NS stages of LDS with loads NS - 1 K-steps ahead of the matrix instructions.
+// 4096x18432x7168: 227 us back to back, 4.8 PFLOP/s (248 with casts between).  Two things bound it.  Waits: of 435 thousand
+// cycles the matrix units are busy for 258 (59%; in a loop on registers 94%), waves wait for data and barriers for 31% of their
+// cycles, to issue for 35%.  Power: random codes run at 1.89 GHz; codes of one value at 2.38, 180 us, in as many cycles.
+// Grouped 256x128 tiles, 8192 rows of 32 experts, N 4096, K 7168: 167 us, 365 thousand cycles at 2.18 GHz, busy for 129 (35%).
 template <int BN_, int BM_, int WN_, int WM_, int NS_>
 struct MainCfg {
     static constexpr int BN = BN_, BM = BM_, WN = WN_, WM = WM_, NS = NS_;
@@ -567,7 +570,7 @@ __global__ __launch_bounds__(C::NT) void gemm_mxfp4_kernel(const MxGemmParams p)
             __builtin_amdgcn_sched_barrier(0);
             // activation fragment j, weight fragment i, half h (four of the eight groups).  An accumulator's two matrix
             // instructions follow each other: FN apart, so that neither would wait for the other, 4096x18432x7168 takes
-            // 263 us instead of 255 (the chip's power is what bounds this kernel, and a chained sum costs less of it).
+            // 263 us instead of 255.
 #pragma unroll
             for (int j = 0; j < FM; ++j) {
                 if (j == FM - 1) {
@@ -797,9 +800,10 @@ static ds3_status launch_main(MxGemmParams p, ds3_dtype ct, int cus, hipStream_t
 
 // The configurations and what a call takes with each: `fixed` + one round of tiles after another, a round being K-steps
 // (of 256) / `wk` steps of `full` us when every workgroup slot has a tile and `alone` us when few have, plus the sums' way
-// out.  Fitted to 9000 shapes (M 1 .. 4096, N 64 .. 24576, K 128 .. 18432, weights from HBM, BF16 output); on 7700 others
-// the one it picks takes 1.030 of the best of 17 configurations' time on average (the best of these eight 1.014), one call
-// in ten more than 1.1 of it, most of those of 5 us, which repeat to 10%.
+// out.  Fitted to 9000 shapes with BF16 output (M 1 .. 4096, N 64 .. 24576, K 128 .. 18432, weights from HBM), before a tile's
+// stores flew on under the next one.  With the kernels as they are the one it picks takes, on 12600 other shapes, 1.015 of the
+// best of these eight's time on average with BF16 output, 1.016 with FP32 (one call in twenty more than 1.1), and 1.030 where the
+// sums are added to what is there, which costs more than `out` says: 1.07 above 20 us, there one call in four more than 1.1.
 struct MxChoice { int bn, bm, wk, per_cu; float fixed, full, alone, out; };
 enum { kMx32x32, kMx64x32, kMx80x32, kMx96x32, kMx64x64two, kMx64x64, kMx128x128, kMx256x256, kMxCfgs };
 constexpr MxChoice kMx[kMxCfgs] = {
@@ -830,7 +834,9 @@ static int mx_dense_choice(int M, int N, int K, int cus) {
     return best;
 }
 
-// Grouped: by the mean rows of an expert (the host knows no more).  Weights from HBM, us with 64x32 / 128x64 / 128x128 /
+// Grouped: by the rows that there is room for, an expert's mean (the host knows no more, the offsets are on the device).  Room
+// for all the rows / eight times as many, us: 32 experts, N 7168, K 2048, 128 rows 46.8 / 47.7, 512 rows 49.9 / 63.7; N 4096,
+// K 7168, 8192 rows 177 / 171.  Weights from HBM, us with 64x32 / 128x64 / 128x128 /
 // 256x128 / 256x256 tiles: 32 experts of 4 rows, N 7168, K 2048 46 / 49 / - / - / -; of 32, N 4096, K 7168 113 / 93 / - / - /
 // -; of 64 - / 122 / 97 / 94 / 106; of 128 - / 158 / 148 / 137 / 119; of 256 - / 236 / 194 / 174 / 172; 8 experts of 512 - /
 // 111 / 101 / 92 / 98; N 7168, K 2048, 32 experts of 64 - / 68 / 59 / 61 / 68, of 256 - / 158 / 124 / 114 / 111.

@@ -425,8 +425,9 @@ static ds3_status launch_status() { return hipGetLastError() == hipSuccess ? DS3
 constexpr int64_t kMaxGrid = (1ll << 24) - 1;          // a grid may have 2^32 threads
 
 // Up to here every workgroup counts all choices itself (65536 of 256 experts 10 us, of which 32 are here 8; the long form
-// takes three launches, of 4, 4 and 13 us at 65536).  Below the second line four choices a load do not pay for the longer
-// kernel (32 choices: 3.4 / 4.6 us, 16384: 8.0 / 7.2, 65536: 17 / 10).
+// takes three launches, of 4, 4 and 13 us at 65536).  In all, 131072 of 256 experts in one launch 13 us, 131080 in three 14,
+// 262144 17, a million 30.  Below the second line four choices a load do not pay for the longer kernel (32 choices: 3.4 / 4.6
+// us, 16384: 8.0 / 7.2, 65536: 17 / 10).
 constexpr int kSortOneLaunch = 131072, kSortPacked = 8192;
 
 template <bool PACKED>
